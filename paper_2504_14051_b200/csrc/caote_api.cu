@@ -13,6 +13,7 @@
 #include "decode_tc.cuh"
 #include "generic_score.cuh"
 #include "greedy.cuh"
+#include "launch.cuh"
 #include "post_evict.cuh"
 #include "prefill_tc.cuh"
 #include "select_compact.cuh"
@@ -21,108 +22,9 @@
 
 namespace caote {
 
-static std::atomic<long long> g_launches{0};
 static std::atomic<long long> g_wait_cycles{2000000000LL};  // CAOTE_OPT_WAIT_CYCLES
 static std::atomic<int> g_side_by_side{1};                  // CAOTE_OPT_SIDE_BY_SIDE: 0 off, 1 when it pays
 static std::atomic<int> g_decode_cluster{0};                // CAOTE_OPT_DECODE_CLUSTER: 0 auto, -1 off, else the size
-static thread_local char g_cuda_error[256] = "";
-
-static int cuda_fail(cudaError_t e, const char* what) {
-  snprintf(g_cuda_error, sizeof(g_cuda_error), "%s: %s", what, cudaGetErrorString(e));
-  return CAOTE_ERR_CUDA;
-}
-#define CAOTE_CUDA(call)                                  \
-  do {                                                    \
-    cudaError_t e__ = (call);                             \
-    if (e__ != cudaSuccess) return cuda_fail(e__, #call); \
-  } while (0)
-
-static int after_launch(const char* name) {
-  g_launches.fetch_add(1, std::memory_order_relaxed);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return cuda_fail(e, name);
-  return CAOTE_OK;
-}
-
-// ---- optional per-kernel tracing: CUDA events recorded on the launching stream around each kernel ----
-struct TraceRec {
-  const char* name;
-  cudaEvent_t a, b;
-};
-static std::atomic<bool> g_trace_on{false};
-static std::mutex g_trace_mu;
-static std::vector<TraceRec> g_trace_pending;
-static std::vector<cudaEvent_t> g_trace_pool;
-
-static cudaEvent_t trace_event() {
-  std::lock_guard<std::mutex> lk(g_trace_mu);
-  if (!g_trace_pool.empty()) {
-    cudaEvent_t e = g_trace_pool.back();
-    g_trace_pool.pop_back();
-    return e;
-  }
-  cudaEvent_t e = nullptr;
-  if (cudaEventCreate(&e) != cudaSuccess) return nullptr;
-  return e;
-}
-
-struct TraceScope {
-  const char* name;
-  cudaStream_t st;
-  cudaEvent_t a = nullptr, b = nullptr;
-  TraceScope(const char* n, cudaStream_t s) : name(n), st(s) {
-    if (!g_trace_on.load(std::memory_order_relaxed)) return;
-    a = trace_event();
-    b = trace_event();
-    if (a && b) cudaEventRecord(a, st);
-  }
-  ~TraceScope() {
-    if (!a || !b) return;
-    cudaEventRecord(b, st);
-    std::lock_guard<std::mutex> lk(g_trace_mu);
-    g_trace_pending.push_back({name, a, b});
-  }
-};
-
-// Launch a kernel (the statement after the stream argument), count it, trace it when tracing is on,
-// and return from the calling function if the launch failed.
-#define CAOTE_LAUNCH(name, st, ...)        \
-  do {                                     \
-    int rc__;                              \
-    {                                      \
-      TraceScope ts__(name, st);           \
-      __VA_ARGS__;                         \
-      rc__ = after_launch(name);           \
-    }                                      \
-    if (rc__ != CAOTE_OK) return rc__;     \
-  } while (0)
-
-// Launch with the programmatic-serialization attribute: the kernel may be scheduled while its predecessor in the
-// stream is still running and waits for it in its first statement (ptx::pdl_wait). Only for kernels that do so.
-// cluster > 1: in clusters of that many CTAs along x.
-template <typename... KArgs, typename... Args>
-static void launch_pdl_clusters(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st,
-                                Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)cluster;
-  at[1].val.clusterDim.y = 1;
-  at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);  // (errors are picked up by after_launch)
-}
-template <typename... KArgs, typename... Args>
-static void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
-  launch_pdl_clusters(kernel, grid, block, smem, 1, st, std::forward<Args>(args)...);
-}
 
 static bool params_ok(const caote_params_t* p) {
   if (!p) return false;
@@ -155,44 +57,6 @@ static Dims make_dims(const caote_params_t* p) {
   d.scale = p->scale;
   d.base_mode = p->base_mode;
   return d;
-}
-
-// The device must be a compute-capability 10.x part; checked once per device.
-static int check_device() {
-  static std::atomic<int> ok[64];
-  int dev = 0;
-  CAOTE_CUDA(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= 64) return CAOTE_ERR_UNSUPPORTED;
-  int st = ok[dev].load(std::memory_order_acquire);
-  if (st == 0) {
-    int major = 0;
-    CAOTE_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
-    st = (major == 10) ? 1 : -1;
-    ok[dev].store(st, std::memory_order_release);
-  }
-  return st == 1 ? CAOTE_OK : CAOTE_ERR_UNSUPPORTED;
-}
-
-// Once per device, kernel and size, not at every launch.
-template <typename KernelT>
-static int allow_smem(KernelT kernel, size_t bytes) {
-  if (bytes <= 48 * 1024) return CAOTE_OK;
-  struct Done { int dev; const void* kernel; size_t bytes; };
-  static std::mutex mu;
-  static std::vector<Done> done;
-  int dev = 0;
-  CAOTE_CUDA(cudaGetDevice(&dev));
-  std::lock_guard<std::mutex> lk(mu);
-  for (Done& d : done)
-    if (d.dev == dev && d.kernel == (const void*)kernel) {
-      if (d.bytes >= bytes) return CAOTE_OK;
-      CAOTE_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-      d.bytes = bytes;
-      return CAOTE_OK;
-    }
-  CAOTE_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-  done.push_back({dev, (const void*)kernel, bytes});
-  return CAOTE_OK;
 }
 
 template <typename T, int D>
@@ -274,24 +138,6 @@ static int launch_small_step(const Dims& dm, const small::Args<T>& sa, int* stat
 }
 
 // ---- single-query fast path ---------------------------------------------------------------------
-typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static TensorMapEncodeFn tensor_map_encoder() {
-  static std::atomic<TensorMapEncodeFn> fn{nullptr};
-  TensorMapEncodeFn f = fn.load(std::memory_order_acquire);
-  if (!f) {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult qr;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qr) == cudaSuccess &&
-        qr == cudaDriverEntryPointSuccess)
-      f = reinterpret_cast<TensorMapEncodeFn>(ptr);
-    fn.store(f, std::memory_order_release);
-  }
-  return f;
-}
-
 // Resident CTAs of the persistent decode kernel on the current device (SMs x CTAs per SM); 0 on error.
 static int decode_grid_limit() {
   static std::atomic<int> cached[64];
@@ -312,8 +158,6 @@ static int decode_grid_limit() {
   }
   return g > 0 ? g : 0;
 }
-
-static inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // Shapes the single-query cluster kernel covers, as long as its clusters hold a unit.
 static bool cluster_shape_ok(const caote_params_t* p) {
@@ -818,26 +662,6 @@ static int launch_prefill_score(const Dims& dm, const void* q, const void* K, co
   };
   const auto run = dm.D == 128 ? pick(std::integral_constant<int, 128>{}) : pick(std::integral_constant<int, 64>{});
   return run(dm, sc, q, K, V, len, base, o, scores, ws, st, vsum, encode);
-}
-
-// The split heuristics of the prefill and any-shape paths look at the SM count: keep it current for this device
-// (cached per device; left at its default when there is no device, e.g. when only sizes are asked for).
-static void refresh_sm_count() {
-  static std::atomic<int> cached[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
-    (void)cudaGetLastError();
-    return;
-  }
-  int n = cached[dev].load(std::memory_order_acquire);
-  if (n == 0) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-      (void)cudaGetLastError();
-      return;
-    }
-    cached[dev].store(n, std::memory_order_release);
-  }
-  g_sm_count = n;
 }
 
 static size_t workspace_bytes(const caote_params_t* p) {
