@@ -63,7 +63,8 @@ typedef enum {
   CAOTE_ERR_TIMEOUT = -4,     /* a bounded device-side wait gave up (status word only)            */
   CAOTE_ERR_BAD_LENGTH = -5,  /* device saw len[b] > cap or 0 < len[b] < n_new (status word only) */
   CAOTE_ERR_OVERFLOW = -6,    /* device saw n_evict > max_evict or len + n_new > cap (status word) */
-  CAOTE_ERR_TOO_LARGE = -7    /* caote_score_static: the shape needs more than CAOTE_STATIC_SCRATCH_BYTES */
+  CAOTE_ERR_TOO_LARGE = -7,   /* caote_score_static: the shape needs more than CAOTE_STATIC_SCRATCH_BYTES */
+  CAOTE_ERR_BAD_PAGE = -8     /* device saw a page index outside the pool (status word only, caote_paged.h) */
 } caote_status_t;
 
 typedef enum { CAOTE_BF16 = 0, CAOTE_F32 = 1 } caote_dtype_t;

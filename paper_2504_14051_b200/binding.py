@@ -19,7 +19,7 @@ BASE_MODES = {"last_query": 0, "chunk_sum": 1, "accum": 2, "external": 3}
 COMPACT_MODES = {"fill": 0, "stable": 1}
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_TIMEOUT, ERR_BAD_LENGTH, ERR_OVERFLOW = 0, -1, -2, -3, -4, -5, -6
-ERR_TOO_LARGE = -7
+ERR_TOO_LARGE, ERR_BAD_PAGE = -7, -8
 STATIC_SCRATCH_BYTES = 16 << 20
 
 
@@ -36,6 +36,25 @@ class Params(ctypes.Structure):
         ("dtype", ctypes.c_int32),
         ("scale", ctypes.c_float),
         ("base_mode", ctypes.c_int32),
+        ("flags", ctypes.c_int32),
+    ]
+
+
+class PagedParams(ctypes.Structure):
+    """Mirror of caote_paged_params_t."""
+
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("total_new", ctypes.c_int32),
+        ("max_new", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("scale", ctypes.c_float),
         ("flags", ctypes.c_int32),
     ]
 
@@ -114,6 +133,17 @@ def lib() -> ctypes.CDLL:
     L.caote_trace_collect.argtypes = [ctypes.POINTER(TraceEntry), i32, ctypes.POINTER(ctypes.c_int32)]
     L.caote_select_evict_greedy.restype = ctypes.c_int
     L.caote_select_evict_greedy.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+    gp, i64 = ctypes.POINTER(PagedParams), ctypes.c_int64
+    L.caote_paged_workspace_bytes.restype = sz
+    L.caote_paged_workspace_bytes.argtypes = [gp]
+    L.caote_prompt_attend.restype = ctypes.c_int
+    L.caote_prompt_attend.argtypes = [gp, vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+    L.caote_paged_append.restype = ctypes.c_int
+    L.caote_paged_append.argtypes = [gp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    L.caote_paged_attend.restype = ctypes.c_int
+    L.caote_paged_attend.argtypes = [gp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.caote_paged_evict.restype = ctypes.c_int
+    L.caote_paged_evict.argtypes = [gp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, i32, vp, vp, sz, vp]
     L.caote_launch_count.restype = ctypes.c_int64
     L.caote_launch_count.argtypes = []
     L.caote_set_option.restype = ctypes.c_int
@@ -291,6 +321,132 @@ def caote_post_evict_output_ws(p, q, K, V, lens, evict_idx, n_evict, o, o_post, 
            _fn.caote_post_evict_output_ws(ctypes.byref(p), _p(q), _p(K), _p(V), _p(lens), _p(evict_idx),
                                           evict_idx.shape[-1], _p(n_evict), _p(o), _p(o_post), _p(workspace),
                                           workspace.numel(), _stream(stream)))
+
+
+# ---- packed prompts and the paged cache (caote_paged.h) ----------------------------------------------------------
+def make_paged_params(batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, total_new, max_new, dtype,
+                      scale) -> PagedParams:
+    """Prompts alone: page_size, n_pages and max_pages are 0."""
+    if isinstance(dtype, torch.dtype):
+        dtype = {torch.bfloat16: BF16, torch.float32: F32}[dtype]
+    return PagedParams(batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, total_new, max_new, dtype,
+                       float(scale), 0)
+
+
+def caote_paged_workspace_bytes(p: PagedParams) -> int:
+    return int(_fn.caote_paged_workspace_bytes(ctypes.byref(p)))
+
+
+def alloc_paged_workspace(p: PagedParams, device) -> torch.Tensor:
+    """A zeroed uint8 workspace of the size the library asks for; one for the largest total_new and max_new serves all."""
+    n = caote_paged_workspace_bytes(p)
+    if n == 0:
+        raise CaoteError("caote_paged_workspace_bytes", ERR_INVALID_ARG)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+_IO = {BF16: torch.bfloat16, F32: torch.float32}
+
+
+# What the library cannot see behind a bare address: a tensor's type, shape, layout and device.
+def _dense(fn, name, t, dtype, shape):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{fn}: {name} has to be a contiguous {dtype} tensor of shape {tuple(shape)}, "
+                         f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _packed(fn, name, t, dtype, shape):
+    """The token stride of a [T, heads, d] tensor that may be a slice of a wider one."""
+    s = t.stride()
+    if t.dtype is not dtype or t.shape != shape or s[2] != 1 or (s[1] != shape[2] and shape[1] != 1) or (s[0] <= 0 and shape[0] > 1):
+        raise ValueError(f"{fn}: {name} has to be a {dtype} tensor of shape {shape} with dense rows, "
+                         f"not {t.dtype} {tuple(t.shape)} with strides {s}")
+    return s[0] if shape[0] > 1 else 0
+
+
+def _here(fn, *tensors):
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != torch._C._cuda_getDevice()):
+            raise ValueError(f"{fn}: every tensor has to be on the current CUDA device, one is on {t.device}")
+
+
+def caote_prompt_attend(p, q, k, v, cu, o, lse, mass, workspace, stream=None):
+    """Causal attention inside packed prompts. lse [T, Hq], mass [T, Hkv]: None if not wanted."""
+    fn, io = "caote_prompt_attend", _IO.get(p.dtype)
+    T, Hq, Hkv, d = p.total_new, p.n_q_heads, p.n_kv_heads, p.head_dim
+    _here(fn, q, k, v, cu, o, lse, mass, workspace)
+    qs, ks = _packed(fn, "q", q, io, (T, Hq, d)), _packed(fn, "k", k, io, (T, Hkv, d))
+    if _packed(fn, "v", v, io, (T, Hkv, d)) != ks:
+        raise ValueError(f"{fn}: k and v need the same token stride")
+    _dense(fn, "cu", cu, torch.int32, (p.batch + 1,))
+    _dense(fn, "o", o, io, (T, Hq, d))
+    if lse is not None:
+        _dense(fn, "lse", lse, torch.float32, (T, Hq))
+    if mass is not None:
+        _dense(fn, "mass", mass, torch.float32, (T, Hkv))
+    _check(fn, _fn.caote_prompt_attend(ctypes.byref(p), _p(q), qs, _p(k), _p(v), ks, _p(cu), _p(o), _p(lse), _p(mass),
+                                       _p(workspace), workspace.numel(), _stream(stream)))
+
+
+def _pools(fn, p, K, V, mass, pos, page_table, lens):
+    shape = (p.n_pages, p.n_kv_heads, p.page_size)
+    io = _IO.get(p.dtype)
+    _dense(fn, "K", K, io, shape + (p.head_dim,))
+    _dense(fn, "V", V, io, shape + (p.head_dim,))
+    if mass is not None:
+        _dense(fn, "mass", mass, torch.float32, shape)
+    if pos is not None:
+        _dense(fn, "pos", pos, torch.int32, shape)
+    _dense(fn, "page_table", page_table, torch.int32, (p.batch, p.max_pages))
+    _dense(fn, "lens", lens, torch.int32, (p.batch,))
+
+
+def caote_paged_append(p, K, V, mass, pos, page_table, lens, n_seen, k_new, v_new, mass_new, cu, workspace, stream=None):
+    """New rows, their positions and their first weights (mass_new [T, Hkv], None: 0) into the pages."""
+    fn, io = "caote_paged_append", _IO.get(p.dtype)
+    T, Hkv, d = p.total_new, p.n_kv_heads, p.head_dim
+    _here(fn, K, V, mass, pos, page_table, lens, n_seen, k_new, v_new, mass_new, cu, workspace)
+    _pools(fn, p, K, V, mass, pos, page_table, lens)
+    ks = _packed(fn, "k_new", k_new, io, (T, Hkv, d))
+    if _packed(fn, "v_new", v_new, io, (T, Hkv, d)) != ks:
+        raise ValueError(f"{fn}: k_new and v_new need the same token stride")
+    if n_seen is not None:
+        _dense(fn, "n_seen", n_seen, torch.int32, (p.batch,))
+    if mass_new is not None:
+        _dense(fn, "mass_new", mass_new, torch.float32, (T, Hkv))
+    _dense(fn, "cu", cu, torch.int32, (p.batch + 1,))
+    _check(fn, _fn.caote_paged_append(ctypes.byref(p), _p(K), _p(V), _p(mass), _p(pos), _p(page_table), _p(lens), _p(n_seen),
+                                      _p(k_new), _p(v_new), ks, _p(mass_new), _p(cu), _p(workspace), workspace.numel(),
+                                      _stream(stream)))
+
+
+def caote_paged_attend(p, q, K, V, mass, page_table, lens, cu, o, lse, workspace, stream=None):
+    """Attention of the new tokens, the last ones of their sequences' pages. mass (None: not wanted) is added to."""
+    fn, io = "caote_paged_attend", _IO.get(p.dtype)
+    T, Hq, d = p.total_new, p.n_q_heads, p.head_dim
+    _here(fn, q, K, V, mass, page_table, lens, cu, o, lse, workspace)
+    qs = _packed(fn, "q", q, io, (T, Hq, d))
+    _pools(fn, p, K, V, mass, None, page_table, lens)
+    _dense(fn, "cu", cu, torch.int32, (p.batch + 1,))
+    _dense(fn, "o", o, io, (T, Hq, d))
+    if lse is not None:
+        _dense(fn, "lse", lse, torch.float32, (T, Hq))
+    _check(fn, _fn.caote_paged_attend(ctypes.byref(p), _p(q), qs, _p(K), _p(V), _p(mass), _p(page_table), _p(lens), _p(cu),
+                                      _p(o), _p(lse), _p(workspace), workspace.numel(), _stream(stream)))
+
+
+def caote_paged_evict(p, K, V, mass, pos, page_table, lens, n_seen, budget, sinks, recent, evict_idx, n_evict, workspace,
+                      stream=None):
+    """The lightest tokens beyond the budget leave the pages; the first `sinks` and the `recent` newest go last."""
+    fn = "caote_paged_evict"
+    _here(fn, K, V, mass, pos, page_table, lens, n_seen, budget, evict_idx, n_evict, workspace)
+    _pools(fn, p, K, V, mass, pos, page_table, lens)
+    for name, t in (("n_seen", n_seen), ("budget", budget), ("n_evict", n_evict)):
+        _dense(fn, name, t, torch.int32, (p.batch,))
+    _dense(fn, "evict_idx", evict_idx, torch.int32, (p.batch, p.n_kv_heads, evict_idx.shape[-1]))
+    _check(fn, _fn.caote_paged_evict(ctypes.byref(p), _p(K), _p(V), _p(mass), _p(pos), _p(page_table), _p(lens), _p(n_seen),
+                                     _p(budget), sinks, recent, _p(evict_idx), evict_idx.shape[-1], _p(n_evict),
+                                     _p(workspace), workspace.numel(), _stream(stream)))
 
 
 def caote_read_status(workspace, stream=None) -> int:

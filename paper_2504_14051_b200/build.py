@@ -9,7 +9,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcaote.so")
-SOURCES = ["caote_api.cu", "decode_step.cu"]
+SOURCES = ["caote_api.cu", "decode_step.cu", "paged_api.cu"]
 
 
 def _nvcc() -> str:
@@ -24,7 +24,8 @@ def _stale() -> bool:
         return True
     t = os.path.getmtime(LIB)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    deps.append(os.path.join(os.path.dirname(HERE), "include", "caote.h"))
+    include = os.path.join(os.path.dirname(HERE), "include")
+    deps += [os.path.join(include, f) for f in os.listdir(include)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -6,6 +6,9 @@ arithmetic happens here.
 
 method: "caote" (Sec. 3.2 score), "fast" (FastCAOTE, Sec. 3.3), "sum_errors" (the per-row errors added up),
 "post_evict" (the "caote" step that also returns the attention output over the retained tokens, Sec. 3.1).
+
+``PagedCache`` is the same for a cache in pages, whose sequences come with prompts and blocks of different lengths and whose
+tokens are evicted by the attention weight they have received (H2O, the base score of Sec. 2).
 """
 from __future__ import annotations
 
@@ -91,6 +94,115 @@ class EvictionCache:
                      self.budget, self.o, self.scores, self.evict_idx, self.n_evict, self.compact_mode,
                      self.workspace, stream)
         return self.o
+
+    def status(self) -> int:
+        return C.caote_read_status(self.workspace)
+
+
+class PagedCache:
+    """Sequences in a pool of pages: prompts are attended whole, later tokens in blocks or one at a time, and the lightest
+    tokens beyond the budget leave after every call. The host knows every length without asking the device: a call appends
+    what it is given and evicts down to the budget.
+
+    A call of `prompt` or `step` takes the new tokens of all sequences packed, q [T, Hq, d], k and v [T, Hkv, d], and how many
+    each sequence has (`new`, 0 for none); it returns o [T, Hq, d]. `o` and `lse` of a call are overwritten by the next one. All work
+    goes to the current stream.
+    """
+
+    def __init__(self, batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_tokens, max_total_new, dtype, budget,
+                 sinks=4, recent=0, scale: Optional[float] = None, device="cuda"):
+        self.device = dev = torch.device(device)
+        self.dtype, self.sinks, self.recent = dtype, sinks, recent
+        self.page_size, self.n_pages, self.max_pages = page_size, n_pages, -(-max_tokens // page_size)
+        self.batch, self.Hq, self.Hkv, self.d = batch, n_q_heads, n_kv_heads, head_dim
+        self.scale = head_dim ** -0.5 if scale is None else scale
+        shape = (n_pages, n_kv_heads, page_size)
+        self.K = torch.zeros(shape + (head_dim,), dtype=dtype, device=dev)
+        self.V = torch.zeros(shape + (head_dim,), dtype=dtype, device=dev)
+        self.mass = torch.zeros(shape, dtype=torch.float32, device=dev)
+        self.pos = torch.zeros(shape, dtype=torch.int32, device=dev)
+        self.page_table = torch.full((batch, self.max_pages), -1, dtype=torch.int32, device=dev)
+        self.lens = torch.zeros((batch,), dtype=torch.int32, device=dev)
+        self.n_seen = torch.zeros((batch,), dtype=torch.int32, device=dev)
+        self.n_evict = torch.zeros((batch,), dtype=torch.int32, device=dev)
+        self.budgets = [budget] * batch if isinstance(budget, int) else [int(x) for x in budget]
+        self.budget = torch.tensor(self.budgets, dtype=torch.int32, device=dev)
+        self.max_total_new = max_total_new
+        self.evict_idx = torch.zeros((batch, n_kv_heads, max_total_new), dtype=torch.int32, device=dev)
+        self.o = torch.zeros((max_total_new, n_q_heads, head_dim), dtype=dtype, device=dev)
+        self.lse = torch.zeros((max_total_new, n_q_heads), dtype=torch.float32, device=dev)
+        self.mass_new = torch.zeros((max_total_new, n_kv_heads), dtype=torch.float32, device=dev)
+        self.workspace = C.alloc_paged_workspace(self._params(max_total_new, max_total_new), dev)
+        self.host_lens = [0] * batch
+        self._pages = [[] for _ in range(batch)]
+        self._free = list(range(n_pages - 1, -1, -1))
+
+    def _params(self, total, most):
+        return C.make_paged_params(self.batch, self.Hq, self.Hkv, self.d, self.page_size, self.n_pages, self.max_pages, total,
+                                   most, self.dtype, self.scale)
+
+    def _begin(self, new):
+        """Pages for the new tokens; (parameters, cu, T)."""
+        new = [int(m) for m in new]
+        T = sum(new)
+        if len(new) != self.batch or min(new) < 0 or not 1 <= T <= self.max_total_new:
+            raise ValueError(f"PagedCache: {self.batch} sequences with 1 to {self.max_total_new} new tokens together, not {new}")
+        need = [-(-(n + m) // self.page_size) for n, m in zip(self.host_lens, new)]
+        if max(need) > self.max_pages:
+            raise ValueError(f"PagedCache: a sequence would need {max(need)} pages of at most {self.max_pages}")
+        more = [max(0, x - len(p)) for x, p in zip(need, self._pages)]
+        if sum(more) > len(self._free):
+            raise ValueError(f"PagedCache: {sum(more)} pages are needed, {len(self._free)} are free")
+        for b, x in enumerate(more):
+            if x:
+                self._pages[b] += [self._free.pop() for _ in range(x)]
+                self.page_table[b, :len(self._pages[b])] = torch.tensor(self._pages[b], dtype=torch.int32)
+        cu = [0]
+        for m in new:
+            cu.append(cu[-1] + m)
+        return new, self._params(T, max(new)), torch.tensor(cu, dtype=torch.int32).to(self.device), T
+
+    def _end(self, p, new):
+        """Eviction down to the budgets; the pages behind the new lengths come free."""
+        after = [min(n + m, max(b, 1)) for n, m, b in zip(self.host_lens, new, self.budgets)]
+        if any(n + m > a for n, m, a in zip(self.host_lens, new, after)):
+            C.caote_paged_evict(p, self.K, self.V, self.mass, self.pos, self.page_table, self.lens, self.n_seen, self.budget,
+                                self.sinks, self.recent, self.evict_idx, self.n_evict, self.workspace)
+        self.host_lens = after
+        for b, n in enumerate(after):
+            keep = -(-n // self.page_size)
+            self._free += self._pages[b][keep:]
+            del self._pages[b][keep:]
+
+    def prompt(self, q, k, v, new):
+        """First tokens of sequences that hold none yet: attended among themselves, then put into pages."""
+        if any(m and n for m, n in zip(new, self.host_lens)):
+            raise ValueError("PagedCache.prompt: a sequence with a prompt already holds tokens")
+        new, p, cu, T = self._begin(new)
+        o, mass = self.o[:T], self.mass_new[:T]
+        C.caote_prompt_attend(p, q, k, v, cu, o, self.lse[:T], mass, self.workspace)
+        C.caote_paged_append(p, self.K, self.V, self.mass, self.pos, self.page_table, self.lens, self.n_seen, k, v, mass, cu,
+                             self.workspace)
+        self._end(p, new)
+        return o
+
+    def step(self, q, k, v, new):
+        """More tokens of some sequences: into the pages, then attended over everything there."""
+        new, p, cu, T = self._begin(new)
+        C.caote_paged_append(p, self.K, self.V, self.mass, self.pos, self.page_table, self.lens, self.n_seen, k, v, None, cu,
+                             self.workspace)
+        o = self.o[:T]
+        C.caote_paged_attend(p, q, self.K, self.V, self.mass, self.page_table, self.lens, cu, o, self.lse[:T], self.workspace)
+        self._end(p, new)
+        return o
+
+    def release(self, b):
+        """Sequence b is done: its pages come free and it may start again with a prompt."""
+        self._free += self._pages[b]
+        self._pages[b] = []
+        self.host_lens[b] = 0
+        self.lens[b] = 0
+        self.n_seen[b] = 0
 
     def status(self) -> int:
         return C.caote_read_status(self.workspace)

@@ -1332,6 +1332,7 @@ const char* caote_status_string(int status) {
     case CAOTE_ERR_BAD_LENGTH: return "a cache length is outside [n_new, capacity]";
     case CAOTE_ERR_OVERFLOW: return "more evictions than max_evict, or an append past capacity";
     case CAOTE_ERR_TOO_LARGE: return "the problem needs more scratch than the built-in array of caote_score_static holds";
+    case CAOTE_ERR_BAD_PAGE: return "a page index is outside the pool";
     default: return "unknown status";
   }
 }

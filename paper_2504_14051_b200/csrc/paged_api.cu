@@ -1,0 +1,225 @@
+// C ABI of the paged cache and of packed prompts (include/caote_paged.h): argument validation, workspace carving, dispatch.
+#include "../../include/caote_paged.h"
+
+#include <type_traits>
+
+#include "launch.cuh"
+#include "paged_common.cuh"
+#include "paged_evict.cuh"
+#include "paged_generic.cuh"
+
+namespace caote {
+namespace paged {
+
+static bool params_ok(const caote_paged_params_t* p, bool pages) {
+  if (!p) return false;
+  if (p->batch < 1 || p->n_kv_heads < 1 || p->n_q_heads < 1 || p->total_new < 1 || p->max_new < 1) return false;
+  if (p->n_q_heads % p->n_kv_heads != 0 || p->n_q_heads / p->n_kv_heads > 16 || p->n_kv_heads > 65535) return false;
+  if (p->max_new > p->total_new || p->flags != 0 || !(p->scale == p->scale)) return false;
+  if ((long long)p->total_new * (p->n_q_heads / p->n_kv_heads) >= (1LL << 31)) return false;
+  if (pages) {
+    if (p->n_pages < 1 || p->max_pages < 1) return false;
+    if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128 && p->page_size != 256) return false;
+    if ((long long)p->n_pages * p->n_kv_heads * p->page_size >= (1LL << 31)) return false;
+    if ((long long)p->max_pages * p->page_size >= (1LL << 31)) return false;
+  }
+  return true;
+}
+static bool params_supported(const caote_paged_params_t* p) {
+  return (p->dtype == CAOTE_BF16 || p->dtype == CAOTE_F32) && (p->head_dim == 64 || p->head_dim == 128);
+}
+// 0 = dense; else at least a dense row, a multiple of 16 bytes.
+static bool stride_ok(const caote_paged_params_t* p, int64_t stride, int heads) {
+  const int64_t row = (int64_t)heads * p->head_dim;
+  return stride == 0 || (stride >= row && stride % (p->dtype == CAOTE_BF16 ? 8 : 4) == 0 && stride < (1LL << 31));
+}
+
+static PDims make_dims(const caote_paged_params_t* p, bool pages, int64_t q_stride, int64_t kv_stride) {
+  PDims d;
+  d.B = p->batch;
+  d.Hq = p->n_q_heads;
+  d.Hkv = p->n_kv_heads;
+  d.G = d.Hq / d.Hkv;
+  d.D = p->head_dim;
+  d.page_shift = 0;
+  d.n_pages = pages ? p->n_pages : 0;
+  d.max_pages = pages ? p->max_pages : 0;
+  if (pages)
+    while ((1 << d.page_shift) < p->page_size) ++d.page_shift;
+  d.T = p->total_new;
+  d.max_new = p->max_new;
+  d.scale = p->scale;
+  d.q_stride = q_stride ? q_stride : (int64_t)d.Hq * d.D;
+  d.kv_stride = kv_stride ? kv_stride : (int64_t)d.Hkv * d.D;
+  return d;
+}
+
+// ---- workspace ------------------------------------------------------------------------------------
+struct Scratch {
+  float* lse2;   // [T, Hq] log2-domain log-sum-exp of every row
+  float* lpart;  // [splits, T, Hq] and
+  float* opart;  // [splits, T, Hq, D]: what the splits of the keys contribute
+};
+constexpr int kMostSplits = 16;
+// Splits are only made where the row blocks of a call fill less than two CTAs per SM, so splits x rows stays below what these
+// hold; a bound that grows with T and does not depend on how the rows lie.
+static long long split_rows(const PDims& dm) {
+  const long long rows = (long long)dm.T * dm.Hq, most = 2LL * g_sm_count * 64;
+  return rows * kMostSplits < most ? rows * kMostSplits : most;
+}
+static size_t carve(const PDims& dm, char* base, Scratch* out) {
+  size_t off = 0;
+  auto take = [&](size_t floats) {
+    float* p = reinterpret_cast<float*>(base + off);
+    off = align_up(off + floats * sizeof(float), 256);
+    return p;
+  };
+  Scratch s;
+  s.lse2 = take((size_t)dm.T * dm.Hq);
+  s.lpart = take((size_t)split_rows(dm));
+  s.opart = take((size_t)split_rows(dm) * dm.D);
+  if (out) *out = s;
+  return off;
+}
+static size_t workspace_bytes(const caote_paged_params_t* p) {
+  refresh_sm_count();
+  return kHeaderBytes + carve(make_dims(p, p->page_size > 0, 0, 0), nullptr, nullptr);
+}
+static bool workspace_ok(const void* workspace, size_t have, size_t need) { return workspace && have >= need && aligned(workspace, 256); }
+
+// ---- the any-type path --------------------------------------------------------------------------------
+template <typename T, int D, bool kPaged>
+static int attend_generic(const PDims& dm, const Seqs& sq, const void* q, const void* K, const void* V, void* o, float* lse, float* mass,
+                          char* ws, cudaStream_t st) {
+  Scratch sc;
+  carve(dm, ws + kHeaderBytes, &sc);
+  int* status = reinterpret_cast<int*>(ws);
+  auto run = [&](auto rpt) -> int {
+    constexpr int RPT = decltype(rpt)::value, kRows = generic::kRows<RPT>;
+    const size_t smem = generic::smem_bytes<D, RPT>();
+    const long long blocks = (long long)dm.T * dm.G / kRows + dm.B;
+    long long splits = 2LL * g_sm_count / (blocks * dm.Hkv);
+    const long long tiles = kPaged ? (((long long)dm.max_pages << dm.page_shift) + generic::kKeys - 1) / generic::kKeys : 0;
+    if (splits > tiles / generic::kLeastTiles) splits = tiles / generic::kLeastTiles;
+    if (splits > kMostSplits) splits = kMostSplits;
+    if (splits < 1) splits = 1;
+    int rc = allow_smem(generic::attend_kernel<T, D, RPT, kPaged>, smem);
+    if (rc) return rc;
+    CAOTE_LAUNCH("paged_attend_generic", st,
+                 launch_pdl(generic::attend_kernel<T, D, RPT, kPaged>, dim3((unsigned)blocks, dm.Hkv, (unsigned)splits), dim3(generic::kThreads),
+                            smem, st, dm, sq, (const T*)q, (const T*)K, (const T*)V, (T*)o, lse, sc.lse2, sc.opart, sc.lpart, status));
+    if (splits > 1)
+      CAOTE_LAUNCH("paged_combine", st,
+                   launch_pdl(generic::combine_kernel<T, D>, dim3((unsigned)(((long long)dm.T * dm.Hq + 7) / 8)), dim3(256), 0, st, dm, sq,
+                              (int)splits, generic::kKeys, generic::kLeastTiles, (const float*)sc.opart, (const float*)sc.lpart, (T*)o, lse,
+                              sc.lse2));
+    if (mass) {
+      const long long kb = kPaged ? (long long)dm.B * tiles : (long long)dm.T / generic::kKeys + dm.B;
+      if (kb > 0x7fffffffLL) return CAOTE_ERR_UNSUPPORTED;
+      rc = allow_smem(generic::mass_kernel<T, D, RPT, kPaged>, smem);
+      if (rc) return rc;
+      CAOTE_LAUNCH("paged_mass_generic", st,
+                   launch_pdl(generic::mass_kernel<T, D, RPT, kPaged>, dim3((unsigned)kb, dm.Hkv), dim3(generic::kThreads), smem, st, dm, sq,
+                              (const T*)q, (const T*)K, (const float*)sc.lse2, mass, status));
+    }
+    return CAOTE_OK;
+  };
+  return generic::rows_per_thread(dm.max_new * dm.G) == 1 ? run(std::integral_constant<int, 1>{}) : run(std::integral_constant<int, 4>{});
+}
+
+template <bool kPaged>
+static int attend(const caote_paged_params_t* p, const PDims& dm, const Seqs& sq, const void* q, const void* K, const void* V, void* o,
+                  float* lse, float* mass, char* ws, cudaStream_t st) {
+  if (p->dtype == CAOTE_F32)
+    return dm.D == 128 ? attend_generic<float, 128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st)
+                       : attend_generic<float, 64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
+  return dm.D == 128 ? attend_generic<__nv_bfloat16, 128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st)
+                     : attend_generic<__nv_bfloat16, 64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
+}
+
+}  // namespace paged
+}  // namespace caote
+
+using namespace caote;
+
+extern "C" {
+
+size_t caote_paged_workspace_bytes(const caote_paged_params_t* p) {
+  if (!p || !paged::params_ok(p, p->page_size != 0) || !paged::params_supported(p)) return 0;
+  return paged::workspace_bytes(p);
+}
+
+int caote_prompt_attend(const caote_paged_params_t* p, const void* q, int64_t q_stride, const void* k, const void* v, int64_t kv_stride,
+                        const int32_t* cu, void* o, float* lse, float* mass, void* workspace, size_t workspace_bytes,
+                        caote_stream_t stream) {
+  if (!paged::params_ok(p, false) || !q || !k || !v || !cu || !o) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::params_supported(p)) return CAOTE_ERR_UNSUPPORTED;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16)) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::stride_ok(p, q_stride, p->n_q_heads) || !paged::stride_ok(p, kv_stride, p->n_kv_heads)) return CAOTE_ERR_INVALID_ARG;
+  refresh_sm_count();
+  const paged::PDims dm = paged::make_dims(p, false, q_stride, kv_stride);
+  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes + paged::carve(dm, nullptr, nullptr))) return CAOTE_ERR_INVALID_ARG;
+  int rc = check_device();
+  if (rc) return rc;
+  return paged::attend<false>(p, dm, paged::Seqs{cu, nullptr, nullptr}, q, k, v, o, lse, mass, (char*)workspace, (cudaStream_t)stream);
+}
+
+int caote_paged_append(const caote_paged_params_t* p, void* K, void* V, float* mass, int32_t* pos, const int32_t* page_table,
+                       int32_t* len, int32_t* n_seen, const void* k_new, const void* v_new, int64_t kv_stride,
+                       const float* mass_new, const int32_t* cu, void* workspace, size_t workspace_bytes, caote_stream_t stream) {
+  if (!paged::params_ok(p, true) || !K || !V || !page_table || !len || !k_new || !v_new || !cu) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::params_supported(p)) return CAOTE_ERR_UNSUPPORTED;
+  if (!aligned(K, 16) || !aligned(V, 16) || !aligned(k_new, 16) || !aligned(v_new, 16)) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::stride_ok(p, kv_stride, p->n_kv_heads)) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes)) return CAOTE_ERR_INVALID_ARG;
+  int rc = check_device();
+  if (rc) return rc;
+  refresh_sm_count();
+  const paged::PDims dm = paged::make_dims(p, true, 0, kv_stride);
+  const int e = p->dtype == CAOTE_BF16 ? 2 : 4, row_bytes = dm.D * e;
+  const long long pieces = (long long)dm.T * dm.Hkv * 2 * (row_bytes / 16);
+  long long ctas = (pieces + 255) / 256;
+  if (ctas > 8LL * g_sm_count) ctas = 8LL * g_sm_count;
+  CAOTE_LAUNCH("paged_append_kernel", (cudaStream_t)stream,
+               launch_pdl(paged::append_kernel, dim3((unsigned)ctas), dim3(256), 0, (cudaStream_t)stream, dm,
+                          paged::Seqs{cu, len, page_table}, row_bytes, dm.kv_stride * e, (char*)K, (char*)V, mass, pos, len, n_seen,
+                          (const char*)k_new, (const char*)v_new, mass_new, (int*)workspace, (int*)workspace + 4));
+  return CAOTE_OK;
+}
+
+int caote_paged_attend(const caote_paged_params_t* p, const void* q, int64_t q_stride, const void* K, const void* V, float* mass,
+                       const int32_t* page_table, const int32_t* len, const int32_t* cu, void* o, float* lse, void* workspace,
+                       size_t workspace_bytes, caote_stream_t stream) {
+  if (!paged::params_ok(p, true) || !q || !K || !V || !page_table || !len || !cu || !o) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::params_supported(p)) return CAOTE_ERR_UNSUPPORTED;
+  if (!aligned(q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(o, 16)) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::stride_ok(p, q_stride, p->n_q_heads)) return CAOTE_ERR_INVALID_ARG;
+  refresh_sm_count();
+  const paged::PDims dm = paged::make_dims(p, true, q_stride, 0);
+  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes + paged::carve(dm, nullptr, nullptr))) return CAOTE_ERR_INVALID_ARG;
+  int rc = check_device();
+  if (rc) return rc;
+  return paged::attend<true>(p, dm, paged::Seqs{cu, len, page_table}, q, K, V, o, lse, mass, (char*)workspace, (cudaStream_t)stream);
+}
+
+int caote_paged_evict(const caote_paged_params_t* p, void* K, void* V, float* mass, int32_t* pos, const int32_t* page_table,
+                      int32_t* len, const int32_t* n_seen, const int32_t* budget, int32_t sinks, int32_t recent, int32_t* evict_idx,
+                      int32_t max_evict, int32_t* n_evict, void* workspace, size_t workspace_bytes, caote_stream_t stream) {
+  if (!paged::params_ok(p, true) || !K || !V || !mass || !pos || !page_table || !len || !n_seen || !budget || !evict_idx || !n_evict)
+    return CAOTE_ERR_INVALID_ARG;
+  if (!paged::params_supported(p)) return CAOTE_ERR_UNSUPPORTED;
+  if (sinks < 0 || recent < 0 || max_evict < 1 || !aligned(K, 16) || !aligned(V, 16)) return CAOTE_ERR_INVALID_ARG;
+  if ((long long)p->batch * p->n_kv_heads >= (1LL << 31)) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes)) return CAOTE_ERR_INVALID_ARG;
+  int rc = check_device();
+  if (rc) return rc;
+  const paged::PDims dm = paged::make_dims(p, true, 0, 0);
+  const int row_bytes = dm.D * (p->dtype == CAOTE_BF16 ? 2 : 4);
+  CAOTE_LAUNCH("paged_evict_kernel", (cudaStream_t)stream,
+               launch_pdl(paged::evict_kernel, dim3(dm.B * dm.Hkv), dim3(paged::kEvictThreads), 0, (cudaStream_t)stream, dm,
+                          paged::Seqs{nullptr, len, page_table}, paged::Pool{(char*)K, (char*)V, mass, pos}, row_bytes, len, n_seen, budget,
+                          sinks, recent, evict_idx, max_evict, n_evict, (int*)workspace, (int*)workspace + 4));
+  return CAOTE_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,99 @@
+// What the kernels of the paged cache and of packed prompts share: where a sequence's rows and tokens lie.
+//
+// New tokens are packed: those of sequence b are rows cu[b] .. cu[b + 1] of q, k_new, v_new, o and lse. Query rows of a
+// (sequence, KV head) pair are numbered r = i * G + g (token i, head g of the group), so that a block of rows is a block of
+// tokens with all heads of the group and every key tile is read once for all of them.
+//
+// A cached token, slot j of sequence b, lies in page table[b, j / page] at row j % page. Pools are [pages, Hkv, page, d] (K,
+// V) and [pages, Hkv, page] (mass, pos): the tokens of a page and a head lie side by side.
+#pragma once
+
+#include "common.cuh"
+
+namespace caote {
+namespace paged {
+
+struct PDims {
+  int B, Hq, Hkv, G, D;
+  int page_shift, n_pages, max_pages;  // pages of 2^page_shift tokens; prompts: no pages (max_pages 0)
+  int T, max_new;                      // new tokens of all sequences, most of one sequence
+  float scale;
+  long long q_stride, kv_stride;  // elements from one packed token to the next
+};
+
+// Where the sequences begin, how long they are.
+struct Seqs {
+  const int* cu;
+  const int* len;    // null: prompts, as long as they have new tokens
+  const int* table;  // null: prompts
+};
+
+struct Seq {
+  int t0, m, n;  // first packed row, new tokens, all tokens; m = 0: nothing to do for this sequence
+};
+
+// A sequence whose numbers do not fit together is left alone (m = 0); `status` (one caller per sequence) gets the code.
+__device__ __forceinline__ Seq sequence(const PDims& dm, const Seqs& sq, int b, int* status = nullptr) {
+  Seq s;
+  const int t1 = sq.cu[b + 1];
+  s.t0 = sq.cu[b];
+  s.m = t1 - s.t0;
+  s.n = sq.len ? sq.len[b] : s.m;
+  if (s.t0 < 0 || t1 < s.t0 || t1 > dm.T || s.m > dm.max_new ||
+      (s.m > 0 && sq.len && (s.n < s.m || s.n > (long long)dm.max_pages << dm.page_shift))) {
+    if (status) set_status(status, CAOTE_ERR_BAD_LENGTH);
+    s.m = 0;
+  }
+  return s;
+}
+
+// Work is numbered over all sequences: sequence b has ceil(what(b) / per) blocks. The sequence that block `index` belongs to
+// and its number in there; false: no such block. For one whole warp, the same result in all lanes.
+template <typename What>
+__device__ __forceinline__ bool locate(int B, int per, int index, What what, int& b_out, int& block_out) {
+  const int lane = threadIdx.x & 31;
+  int base = 0;
+  for (int b0 = 0; b0 < B; b0 += 32) {
+    const int b = b0 + lane;
+    const int mine = b < B ? (what(b) + per - 1) / per : 0;
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += t;
+    }
+    const unsigned reach = __ballot_sync(0xffffffffu, index < base + incl);
+    if (reach) {
+      const int f = __ffs((int)reach) - 1;
+      b_out = b0 + f;
+      block_out = index - (base + __shfl_sync(0xffffffffu, incl - mine, f));
+      return true;
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return false;
+}
+
+// Row of the pools' [pages * Hkv * page] rows that holds slot j of sequence b for KV head h. A page outside the pool is
+// recorded and read as page 0: its sequence's results mean nothing then, but nothing is read out of bounds.
+__device__ __forceinline__ size_t pool_row(const PDims& dm, const Seqs& sq, int b, int h, int j, int* status) {
+  int page = __ldg(sq.table + (size_t)b * dm.max_pages + (j >> dm.page_shift));
+  if ((unsigned)page >= (unsigned)dm.n_pages) {
+    set_status(status, CAOTE_ERR_BAD_PAGE);
+    page = 0;
+  }
+  return (((size_t)page * dm.Hkv + h) << dm.page_shift) + (j & ((1 << dm.page_shift) - 1));
+}
+
+// Splits of a sequence's key tiles (device and combine kernel agree on it): `per` tiles each, `count` of them.
+__device__ __forceinline__ void key_splits(int tiles, int most, int least_tiles, int& per, int& count) {
+  int ns = tiles / least_tiles;
+  ns = ns < 1 ? 1 : (ns > most ? most : ns);
+  per = (tiles + ns - 1) / ns;
+  count = (tiles + per - 1) / per;
+}
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+}  // namespace paged
+}  // namespace caote
