@@ -7,6 +7,7 @@
 #include "paged_common.cuh"
 #include "paged_evict.cuh"
 #include "paged_generic.cuh"
+#include "paged_tc.cuh"
 
 namespace caote {
 namespace paged {
@@ -61,10 +62,10 @@ struct Scratch {
   float* opart;  // [splits, T, Hq, D]: what the splits of the keys contribute
 };
 constexpr int kMostSplits = 16;
-// Splits are only made where the row blocks of a call fill less than two CTAs per SM, so splits x rows stays below what these
-// hold; a bound that grows with T and does not depend on how the rows lie.
+// Splits are only made where the row blocks of a call leave room (two CTAs of 64 rows per SM, or one of 256), so splits x rows
+// stays below what these hold; a bound that grows with T and does not depend on how the rows lie.
 static long long split_rows(const PDims& dm) {
-  const long long rows = (long long)dm.T * dm.Hq, most = 2LL * g_sm_count * 64;
+  const long long rows = (long long)dm.T * dm.Hq, most = 256LL * g_sm_count;
   return rows * kMostSplits < most ? rows * kMostSplits : most;
 }
 static size_t carve(const PDims& dm, char* base, Scratch* out) {
@@ -127,12 +128,82 @@ static int attend_generic(const PDims& dm, const Seqs& sq, const void* q, const 
   return generic::rows_per_thread(dm.max_new * dm.G) == 1 ? run(std::integral_constant<int, 1>{}) : run(std::integral_constant<int, 4>{});
 }
 
+// ---- the tensor-core path -------------------------------------------------------------------------------
+static int encode_failed(CUresult r) {
+  snprintf(g_cuda_error, sizeof(g_cuda_error), "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+  return CAOTE_ERR_CUDA;
+}
+// q [T, Hq, d] as boxes of 64 channels x G heads x 128 / G tokens.
+static int encode_q(const PDims& dm, const void* q, CUtensorMap* tm) {
+  const cuuint64_t dim[3] = {(cuuint64_t)dm.D, (cuuint64_t)dm.Hq, (cuuint64_t)dm.T};
+  const cuuint64_t stride[2] = {(cuuint64_t)dm.D * 2, (cuuint64_t)dm.q_stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)dm.G, (cuuint32_t)(tcore::kTile / dm.G)}, step[3] = {1, 1, 1};
+  const CUresult r = tensor_map_encoder()(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dim, stride, box, step,
+                                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? CAOTE_OK : encode_failed(r);
+}
+// K or V as boxes of 64 channels x `box` tokens: the pool's rows, or a prompt's rows with their heads side by side.
+static int encode_keys(const PDims& dm, const void* x, bool pages, int box_tokens, CUtensorMap* tm) {
+  const cuuint64_t dim[2] = {(cuuint64_t)dm.D * (pages ? 1 : dm.Hkv),
+                             pages ? (cuuint64_t)dm.n_pages * dm.Hkv << dm.page_shift : (cuuint64_t)dm.T};
+  const cuuint64_t stride[1] = {(cuuint64_t)(pages ? dm.D : dm.kv_stride) * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_tokens}, step[2] = {1, 1};
+  const CUresult r = tensor_map_encoder()(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(x), dim, stride, box, step,
+                                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? CAOTE_OK : encode_failed(r);
+}
+
+template <int D, bool kPaged>
+static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void* K, const void* V, void* o, float* lse, float* mass, char* ws,
+                     cudaStream_t st) {
+  if (!tensor_map_encoder()) {
+    snprintf(g_cuda_error, sizeof(g_cuda_error), "cuTensorMapEncodeTiled is not to be had");
+    return CAOTE_ERR_CUDA;
+  }
+  Scratch sc;
+  carve(dm, ws + kHeaderBytes, &sc);
+  int* status = reinterpret_cast<int*>(ws);
+  const int box = kPaged && dm.page_shift < 7 ? 1 << dm.page_shift : tcore::kTile;
+  CUtensorMap tmQ, tmK, tmV;
+  int rc = encode_q(dm, q, &tmQ);
+  if (!rc) rc = encode_keys(dm, K, kPaged, box, &tmK);
+  if (!rc) rc = encode_keys(dm, V, kPaged, box, &tmV);
+  if (!rc) rc = allow_smem(tcore::attend_kernel<D, kPaged>, tcore::attend_smem<D>());
+  if (!rc && mass) rc = allow_smem(tcore::mass_kernel<D, kPaged>, tcore::mass_smem<D>());
+  if (rc) return rc;
+  const int tok = tcore::kTile / dm.G;
+  const long long blocks = dm.T / (2 * tok) + dm.B, cap = (long long)dm.max_pages << dm.page_shift;
+  long long splits = g_sm_count / (blocks * dm.Hkv);
+  if (splits > cap / tcore::kTile / tcore::kLeastTiles) splits = cap / tcore::kTile / tcore::kLeastTiles;
+  if (splits > kMostSplits) splits = kMostSplits;
+  if (splits < 1) splits = 1;
+  const long long key_blocks = kPaged ? (cap + tcore::kKeys - 1) / tcore::kKeys * dm.B : (long long)dm.T / tcore::kKeys + dm.B;
+  if (blocks > 0x7fffffffLL || key_blocks > 0x7fffffffLL) return CAOTE_ERR_UNSUPPORTED;
+  CAOTE_LAUNCH("paged_attend_kernel", st,
+               launch_pdl(tcore::attend_kernel<D, kPaged>, dim3((unsigned)blocks, dm.Hkv, (unsigned)splits), dim3(tcore::kAttendThreads),
+                          tcore::attend_smem<D>(), st, tmQ, tmK, tmV, dm, sq, box, (__nv_bfloat16*)o, lse, sc.lse2, sc.opart, sc.lpart, status));
+  if (splits > 1)
+    CAOTE_LAUNCH("paged_combine", st,
+                 launch_pdl(generic::combine_kernel<__nv_bfloat16, D>, dim3((unsigned)(((long long)dm.T * dm.Hq + 7) / 8)), dim3(256), 0, st, dm,
+                            sq, (int)splits, tcore::kTile, tcore::kLeastTiles, (const float*)sc.opart, (const float*)sc.lpart,
+                            (__nv_bfloat16*)o, lse, sc.lse2));
+  if (mass)
+    CAOTE_LAUNCH("paged_mass_kernel", st,
+                 launch_pdl(tcore::mass_kernel<D, kPaged>, dim3((unsigned)key_blocks, dm.Hkv), dim3(tcore::kMassThreads), tcore::mass_smem<D>(),
+                            st, tmQ, tmK, dm, sq, box, (const float*)sc.lse2, mass, status));
+  return CAOTE_OK;
+}
+
 template <bool kPaged>
 static int attend(const caote_paged_params_t* p, const PDims& dm, const Seqs& sq, const void* q, const void* K, const void* V, void* o,
                   float* lse, float* mass, char* ws, cudaStream_t st) {
   if (p->dtype == CAOTE_F32)
     return dm.D == 128 ? attend_generic<float, 128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st)
                        : attend_generic<float, 64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
+  if (dm.scale > 0.f)  // (the tensor-core kernels take the largest product for the largest logit)
+    return dm.D == 128 ? attend_tc<128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st) : attend_tc<64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
   return dm.D == 128 ? attend_generic<__nv_bfloat16, 128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st)
                      : attend_generic<__nv_bfloat16, 64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
 }

@@ -1,0 +1,531 @@
+// Attention of packed rows over prompts or pages on the tensor cores (tcgen05 + TMEM): bf16, head_dim 64 or 128.
+//
+//   attend_kernel   rows x keys. A CTA owns two blocks of up to 128 query rows of a (sequence, KV head) pair (a block: 128 / G
+//                   tokens with all G heads) and walks the keys that they see in tiles of 128, K and V of a tile read once for
+//                   both blocks. S = Q K^T into TMEM; a thread per row takes its 128 logits out of TMEM, keeps running maximum
+//                   and sum, and writes its numerators P as bf16 over the S it came from; O += P V with P as the TMEM-side A
+//                   operand. The two blocks take turns: while one's logits are being exponentiated, the other's products run.
+//   mass_kernel     keys x rows. A CTA owns 256 keys of a pair and walks the rows that see them: S^T = K Q^T into TMEM, one key
+//                   per lane, so that a thread sums 2^(s - lse) over the rows of its own key without any exchange.
+//
+// Roundings: P is rounded to bf16 once (2^-9 of each weight at most, half of that on average, of random sign); o, of which it
+// is a weighted sum, is rounded to bf16 itself, so o's error against 64 bits is sqrt(2) of what the output's type costs.
+// Maximum, sum, O, lse and mass are fp32; the sum takes the numerators before they are rounded.
+//
+// Operands come by TMA as boxes of 64 channels with the 128-byte swizzle: of q a box of all heads of the group x 128 / G tokens,
+// of K and V a box per page (pages of 16 tokens: eight per tile), by the lanes of a warp side by side. Every mbarrier wait is
+// bounded; one that runs out records CAOTE_ERR_TIMEOUT and the thread carries on in bounds.
+#pragma once
+
+#include <cuda.h>
+
+#include "paged_common.cuh"
+#include "ptx.cuh"
+#include "tc.cuh"
+
+namespace caote {
+namespace paged {
+namespace tcore {
+
+using namespace caote::tc;
+using ptx::tma_load_3d;
+
+constexpr int kLeastTiles = 4;  // key tiles per split
+template <int D>
+constexpr int kKStages = D == 128 ? 2 : 4;
+template <int D>
+constexpr int kVStages = D == 128 ? 3 : 4;
+constexpr int kAttendThreads = 256 + 96;  // a thread per row of two blocks; warps for products, K copies, V copies
+template <int D>
+constexpr size_t attend_smem() { return 1024 + (size_t)(2 + kKStages<D> + kVStages<D>) * kTileBytesOf<D> + 512; }
+
+// Tiles of 128 keys come as boxes of `box` tokens: min(page, 128), prompts 128. Lane l of a warp copies box l of a tile.
+// The page of this lane's box of the tile at slot j0 (of no meaning behind the length).
+template <bool kPaged>
+__device__ __forceinline__ int page_of(const PDims& dm, const Seqs& sq, int b, int n, int j0, int box, int* status) {
+  if (!kPaged) return 0;
+  const int lane = threadIdx.x & 31, j = j0 + lane * box;
+  if (lane * box >= kTile || j >= n) return 0;
+  int id = __ldg(sq.table + (size_t)b * dm.max_pages + (j >> dm.page_shift));
+  if ((unsigned)id >= (unsigned)dm.n_pages) {
+    set_status(status, CAOTE_ERR_BAD_PAGE);
+    id = 0;
+  }
+  return id;
+}
+template <bool kPaged>
+__device__ __forceinline__ int boxes_of(const Seq& s, int j0, int box) { return kPaged ? (min(kTile, s.n - j0) + box - 1) / box : 1; }
+// Copies a tile of K or V into a stage, bytes announced by the caller; the whole warp.
+template <int D, bool kPaged>
+__device__ __forceinline__ void copy_keys(const PDims& dm, const CUtensorMap* tm, const Seq& s, int h, int j0, int box, int id, char* dst,
+                                          uint64_t* bar) {
+  const int lane = threadIdx.x & 31;
+  if (lane < boxes_of<kPaged>(s, j0, box)) {
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) {
+      if (kPaged)
+        tma_load_2d(dst + x * kHalfBytes + lane * box * 128, tm, 64 * x,
+                    ((id * dm.Hkv + h) << dm.page_shift) + ((j0 + lane * box) & ((1 << dm.page_shift) - 1)), bar);
+      else
+        tma_load_2d(dst + x * kHalfBytes, tm, h * D + 64 * x, s.t0 + j0, bar);
+    }
+  }
+  __syncwarp();
+}
+
+// grid = (pairs of row blocks of all sequences, Hkv, splits). lse2 [T, Hq]: the rows' statistics for the mass; with more than one
+// split opart, lpart as in generic::attend_kernel.
+template <int D, bool kPaged>
+__global__ void __launch_bounds__(kAttendThreads, 1)
+attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+              PDims dm, Seqs sq, int box, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ lse2,
+              float* __restrict__ opart, float* __restrict__ lpart, int* status) {
+  constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16, kKS = kKStages<D>, kVS = kVStages<D>;
+  ptx::pdl_wait();
+  ptx::pdl_trigger();
+  extern __shared__ char smem_raw[];
+  // (aligned by an offset into the array: the pointer keeps its address space)
+  char* sm = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  char* Qs = sm;                  // [2]
+  char* Ks = Qs + 2 * kTB;        // [kKS]
+  char* Vs = Ks + kKS * kTB;      // [kVS]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(Vs + kVS * kTB);
+  uint64_t *q_bar = &bars[0], *k_bar = &bars[1], *v_bar = k_bar + kKS, *k_free = v_bar + kVS, *v_free = k_free + kKS,
+           *s_bar = v_free + kVS, *o_bar = s_bar + 2, *p_bar = o_bar + 2;  // p_bar: [block][part]
+  constexpr int kBars1 = 1 + 2 * (kKS + kVS) + 4;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars1 + 4);
+  int* where = reinterpret_cast<int*>(tmem_slot + 1);
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index(), h = blockIdx.y, split = blockIdx.z;
+  const int tok = kTile / dm.G;  // tokens per row block
+  if (warp == 0) {
+    int b = -1, block = 0;
+    if (!locate(dm.B, 2 * tok, blockIdx.x, [&](int x) { return sequence(dm, sq, x).m; }, b, block)) b = -1;
+    if (lane == 0) { where[0] = b; where[1] = block; }
+  } else if (warp == 1 && blockIdx.x == 0 && h == 0 && split == 0) {
+    for (int x = lane; x < dm.B; x += 32) sequence(dm, sq, x, status);
+  }
+  if (tid == 0) {
+    for (int i = 0; i < kBars1; ++i) mbar_init(&bars[i], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&p_bar[i], 4);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const int b = where[0];
+  if (b < 0) return;
+  const Seq s = sequence(dm, sq, b);
+  const int first = s.n - s.m;  // token i sees slots up to first + i
+  // blocks with most keys first: the last CTAs of a launch are short ones
+  const int i0 = ((s.m + 2 * tok - 1) / (2 * tok) - 1 - where[1]) * 2 * tok;
+  int per, count;
+  key_splits((s.n + kTile - 1) / kTile, gridDim.z, kLeastTiles, per, count);
+  if (split >= count) return;
+  // this CTA's tiles [kt0, kt0 + c) for either block
+  const int kt0 = split * per;
+  const int c0 = min(per, (first + min(i0 + tok, s.m) - 1) / kTile + 1 - kt0);
+  const int c1 = i0 + tok < s.m ? min(per, (first + min(i0 + 2 * tok, s.m) - 1) / kTile + 1 - kt0) : 0;
+  const int tiles = max(max(c0, c1), 0);
+
+  if (warp == 0) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  // columns: S (and P) of block i at 128 i, O at 256 + 128 i
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp >= 9) {
+    // =============================== copies: warp 9 Q and K, warp 10 V ===============================
+    const bool is_v = warp == 10;
+    const CUtensorMap* tm = is_v ? &tmV : &tmK;
+    char* ring = is_v ? Vs : Ks;
+    uint64_t *full = is_v ? v_bar : k_bar, *free = is_v ? v_free : k_free;
+    const int stages = is_v ? kVS : kKS;
+    if (!is_v && lane == 0 && tiles > 0) {
+      const int blocks = c1 > 0 ? 2 : 1;
+      mbar_expect_tx(q_bar, blocks * kBoxes * tok * dm.G * 128);
+      for (int i = 0; i < blocks; ++i)
+#pragma unroll
+        for (int x = 0; x < kBoxes; ++x)
+          tma_load_3d(Qs + i * kTB + x * kHalfBytes, &tmQ, 64 * x, h * dm.G, s.t0 + i0 + i * tok, q_bar);
+    }
+    int id = page_of<kPaged>(dm, sq, b, s.n, kt0 * kTile, box, status);
+    int st = 0, round = 0;
+    for (int kt = 0; kt < tiles; ++kt) {
+      const int j0 = (kt0 + kt) * kTile;
+      const int next = page_of<kPaged>(dm, sq, b, s.n, j0 + kTile, box, status);
+      if (round > 0) mbar_wait_idle(&free[st], (round - 1) & 1, status);
+      if (lane == 0) mbar_expect_tx(&full[st], boxes_of<kPaged>(s, j0, box) * box * D * 2);
+      __syncwarp();
+      copy_keys<D, kPaged>(dm, tm, s, h, j0, box, id, ring + st * kTB, &full[st]);
+      id = next;
+      if (++st == stages) { st = 0; ++round; }
+    }
+  } else if (warp == 8) {
+    // =============================== products (one lane) ===============================
+    if (ptx::elect_one() && tiles > 0) {
+      constexpr uint32_t kIdescS = instr_desc_n(false, kTile), kIdescO = instr_desc_n(true, D);
+      const uint64_t qdesc0 = smem_desc(smem_u32(Qs), 16, 1024), kdesc0 = smem_desc(smem_u32(Ks), 16, 1024),
+                     vdesc0 = smem_desc(smem_u32(Vs), kHalfBytes, 1024);
+      auto issue_s = [&](int i, int kt) {  // S of block i and tile kt
+        const int st = kt % kKS;
+        mbar_wait(&k_bar[st], (kt / kKS) & 1, status);
+        tc_fence_after();
+        const uint64_t qd = qdesc0 + (uint64_t)((i * kTB) >> 4), kd = kdesc0 + (uint64_t)((st * kTB) >> 4);
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) umma(tmem + i * 128, qd + k_major_step(ks), kd + k_major_step(ks), kIdescS, ks > 0);
+        umma_commit(&s_bar[i]);
+        // (the last block that reads this K hands its stage back, if anyone waits for it)
+        if (kt + kKS < tiles && (i == 1 || kt >= c1)) umma_commit(&k_free[st]);
+      };
+      mbar_wait(q_bar, 0, status);
+      if (c0 > 0) issue_s(0, 0);
+      if (c1 > 0) issue_s(1, 0);
+      for (int kt = 0; kt < tiles; ++kt) {
+        const int st = kt % kVS;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int c = i ? c1 : c0;
+          if (kt >= c) continue;
+          mbar_wait(&v_bar[st], (kt / kVS) & 1, status);
+          const uint64_t vd = vdesc0 + (uint64_t)((st * kTB) >> 4);
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {  // 64 keys each, as the rows hand them over
+            mbar_wait(&p_bar[2 * i + part], kt & 1, status);
+            tc_fence_after();
+#pragma unroll
+            for (int ks = 4 * part; ks < 4 * part + 4; ++ks)
+              umma_ts(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, vd + mn_major_step(ks), kIdescO, kt > 0 || ks > 0);
+          }
+          if (kt + kVS < tiles && (i == 1 || kt >= c1)) umma_commit(&v_free[st]);
+          umma_commit(&o_bar[i]);
+          // (in the order of issue: the product above has read P before this one overwrites it)
+          if (kt + 1 < c) issue_s(i, kt + 1);
+        }
+      }
+    }
+  } else {
+    // =============================== a thread per query row ===============================
+    const int i = warp >> 2, row = tid & 127, c = i ? c1 : c0;
+    const int tkn = i0 + i * tok + row / dm.G;
+    const bool valid = row < tok * dm.G && tkn < s.m;
+    const int vis = valid ? first + tkn + 1 : s.n;       // keys this row sees
+    const int plain = first + i0 + i * tok + 1;          // ... and every row of the block
+    const float scale2 = dm.scale * kLog2e;
+    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + i * 128, t_o = t_s + 256;
+    float m_ref = -INFINITY, l = 0.f;
+    for (int kt = 0; kt < c; ++kt) {
+      const int j0 = (kt0 + kt) * kTile;
+      mbar_wait(&s_bar[i], kt & 1, status);
+      tc_fence_after();
+      float sv[2][64];
+      tmem_ld64(t_s, sv[0]);
+      tmem_ld64(t_s + 64, sv[1]);
+      if (j0 + kTile > plain) {
+        const int lim = vis - j0;
+#pragma unroll
+        for (int e = 0; e < 128; ++e) sv[e >> 6][e & 63] = e < lim ? sv[e >> 6][e & 63] : -INFINITY;
+      }
+      float mx;
+      {
+        float pm[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pm[e] = fmaxf(sv[0][e], sv[0][e + 8]);
+#pragma unroll
+        for (int e = 16; e < 128; e += 16) {
+#pragma unroll
+          for (int f = 0; f < 8; ++f) pm[f] = fmaxf(fmaxf(pm[f], sv[e >> 6][(e & 63) + f]), sv[e >> 6][(e & 63) + 8 + f]);
+        }
+        mx = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), fmaxf(fmaxf(pm[4], pm[5]), fmaxf(pm[6], pm[7]))) * scale2;
+      }
+      // the reference moves only when a logit exceeds it by more than 8 (numerators up to 256 in between)
+      const bool need = mx > m_ref + 8.f;
+      float corr = 1.f;
+      if (need) {
+        corr = ptx::fast_exp2(m_ref - mx);
+        m_ref = mx;
+        l *= corr;
+      }
+      if (kt > 0 && __any_sync(0xffffffffu, need)) {
+        // (S of this tile was formed behind O += P V of the tile before)
+#pragma unroll 1
+        for (int cc = 0; cc < D / 16; ++cc) {
+          uint32_t v[16];
+          tmem_ld16_issue(t_o + cc * 16, v);
+          tmem_ld16_wait(v);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * corr);
+          tmem_st16u(t_o + cc * 16, v);
+        }
+      }
+      const int n_valid = s.n - j0;
+      if (n_valid < kTile) {
+        // V rows behind the length hold anything: they become zeros, so that 0 * NaN cannot reach O. (Both blocks' rows write
+        // the same zeros, each before its own products.)
+        mbar_wait(&v_bar[kt % kVS], (kt / kVS) & 1, status);
+        if (row >= n_valid) {
+          char* vt = Vs + (kt % kVS) * kTB;
+#pragma unroll
+          for (int x = 0; x < D / 8; ++x)
+            *reinterpret_cast<uint4*>(vt + (x >> 3) * kHalfBytes + row * 128 + (((x & 7) ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        ptx::fence_async_smem();
+      }
+      const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
+      const float2 scale22 = make_float2(scale2, scale2), neg2 = make_float2(neg, neg);
+      float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        uint32_t pk[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float2 x = __ffma2_rn(make_float2(sv[part][2 * e], sv[part][2 * e + 1]), scale22, neg2);
+          const float2 p = make_float2(ptx::fast_exp2(x.x), ptx::fast_exp2(x.y));
+          ls[e & 1] = __fadd2_rn(ls[e & 1], p);
+          pk[e] = pack_bf16(p.x, p.y);
+        }
+        tmem_st32u(t_s + 32 * part, pk);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_bar[2 * i + part]);
+      }
+      l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+    }
+    if (c > 0) {
+      mbar_wait(&o_bar[i], (c - 1) & 1, status);
+      tc_fence_after();
+    }
+    // ---- the row's output and statistic ----
+    const float inv = l > 0.f ? 1.f / l : 0.f, stat = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
+    const size_t at = (size_t)(s.t0 + tkn) * dm.Hq + h * dm.G + row % dm.G;
+    if (count == 1) {
+      if (valid) {
+        lse2[at] = stat;
+        if (lse) lse[at] = stat * kLn2;
+      }
+#pragma unroll
+      for (int cc = 0; cc < D / 32; ++cc) {
+        float v[32];
+        tmem_ld32(t_o + cc * 32, v);
+        if (valid) {
+          uint4* dst = reinterpret_cast<uint4*>(o + at * D + cc * 32);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            dst[e] = make_uint4(pack_bf16(v[8 * e] * inv, v[8 * e + 1] * inv), pack_bf16(v[8 * e + 2] * inv, v[8 * e + 3] * inv),
+                                pack_bf16(v[8 * e + 4] * inv, v[8 * e + 5] * inv), pack_bf16(v[8 * e + 6] * inv, v[8 * e + 7] * inv));
+        }
+      }
+    } else {
+      const size_t slot = (size_t)split * dm.T * dm.Hq + at;
+      if (valid) lpart[slot] = stat;
+#pragma unroll
+      for (int cc = 0; cc < D / 32; ++cc) {
+        float v[32];
+        if (c > 0) tmem_ld32(t_o + cc * 32, v);
+        if (valid && c > 0) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<float4*>(opart + slot * D + cc * 32 + e) = make_float4(v[e] * inv, v[e + 1] * inv, v[e + 2] * inv, v[e + 3] * inv);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+// ---- the weight that every key received ------------------------------------------------------------------
+constexpr int kKeys = 2 * kTile;                       // keys per CTA
+constexpr int kKeyThreads = 2 * kKeys;                 // two threads per key: 64 rows of a row block each
+constexpr int kMassThreads = kKeyThreads + 96;         // + products, K and Q copies, statistics
+constexpr int kQStages = 3, kStatStages = 4;
+template <int D>
+constexpr size_t mass_smem() { return 1024 + (size_t)(2 + kQStages) * kTileBytesOf<D> + (kStatStages * kTile + kKeys) * sizeof(float) + 512; }
+
+// Adds the weights 2^(s * scale2 + stat) of a key in 16 rows to acc; two of eight exponentials on the FMA pipe. masked: only rows
+// [lo, hi) of them count (the others' products may be anything).
+__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], const float4 (&st)[4], float scale2, bool masked, int lo, int hi, float2 (&acc)[2]) {
+  const float2 scale22 = make_float2(scale2, scale2);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1])), scale22, make_float2(st[k].x, st[k].y));
+    float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3])), scale22, make_float2(st[k].z, st[k].w));
+    if (masked) {
+      if (4 * k < lo || 4 * k >= hi) a.x = -INFINITY;
+      if (4 * k + 1 < lo || 4 * k + 1 >= hi) a.y = -INFINITY;
+      if (4 * k + 2 < lo || 4 * k + 2 >= hi) b.x = -INFINITY;
+      if (4 * k + 3 < lo || 4 * k + 3 >= hi) b.y = -INFINITY;
+    }
+    acc[0] = __fadd2_rn(acc[0], make_float2(ptx::fast_exp2(a.x), ptx::fast_exp2(a.y)));
+    if (k & 1) b = poly_exp2x2(b);
+    else b = make_float2(ptx::fast_exp2(b.x), ptx::fast_exp2(b.y));
+    acc[1] = __fadd2_rn(acc[1], b);
+  }
+}
+
+// grid = (blocks of 256 keys of all sequences, Hkv).
+template <int D, bool kPaged>
+__global__ void __launch_bounds__(kMassThreads, 1)
+mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, PDims dm, Seqs sq, int box,
+            const float* __restrict__ lse2, float* __restrict__ mass, int* status) {
+  constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16;
+  ptx::pdl_wait();
+  ptx::pdl_trigger();
+  extern __shared__ char smem_raw[];
+  char* sm = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  char* Ks = sm;                                                      // [2]
+  char* Qs = Ks + 2 * kTB;                                            // [kQStages]
+  float* Ss = reinterpret_cast<float*>(Qs + kQStages * kTB);          // [kStatStages][kTile] minus the rows' lse2
+  float* half = Ss + kStatStages * kTile;                             // [kKeys]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(half + kKeys);
+  uint64_t *k_bar = &bars[0], *q_bar = &bars[1], *q_free = q_bar + kQStages, *s_bar = q_free + kQStages, *st_bar = s_bar + 2,
+           *s_free = st_bar + kStatStages, *st_free = s_free + 2;
+  constexpr int kBars1 = 1 + 2 * kQStages + 2 + kStatStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars1 + 2 + kStatStages);
+  int* where = reinterpret_cast<int*>(tmem_slot + 1);
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index(), h = blockIdx.y;
+  if (warp == 0) {
+    int b = -1, block = 0;
+    if (!locate(dm.B, kKeys, blockIdx.x, [&](int x) { const Seq s = sequence(dm, sq, x); return s.m > 0 ? s.n : 0; }, b, block)) b = -1;
+    if (lane == 0) { where[0] = b; where[1] = block; }
+  }
+  if (tid == 0) {
+    for (int i = 0; i < kBars1; ++i) mbar_init(&bars[i], 1);
+    for (int i = kBars1; i < kBars1 + 2 + kStatStages; ++i) mbar_init(&bars[i], kKeyThreads / 32);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const int b = where[0], j0 = where[1] * kKeys;
+  if (b < 0) return;
+  const Seq s = sequence(dm, sq, b);
+  const int first = s.n - s.m, tok = kTile / dm.G;
+  // row blocks that see any of the keys
+  const int rb0 = max(0, j0 - first) / tok, blocks = (s.m + tok - 1) / tok - rb0;
+  const int tiles = j0 + kTile < s.n ? 2 : 1;
+
+  if (warp == 0) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;  // S^T of key tile kk, buffer buf: columns [kk * 256 + buf * 128, + 128)
+
+  if (warp == 17) {
+    // =============================== copies of K and of the Q blocks ===============================
+    if (lane == 0) mbar_expect_tx(k_bar, (boxes_of<kPaged>(s, j0, box) + (tiles == 2 ? boxes_of<kPaged>(s, j0 + kTile, box) : 0)) * box * D * 2);
+    __syncwarp();
+    for (int kk = 0; kk < tiles; ++kk) {
+      const int id = page_of<kPaged>(dm, sq, b, s.n, j0 + kk * kTile, box, status);
+      copy_keys<D, kPaged>(dm, &tmK, s, h, j0 + kk * kTile, box, id, Ks + kk * kTB, k_bar);
+    }
+    if (ptx::elect_one()) {
+      for (int rb = 0; rb < blocks; ++rb) {
+        const int st = rb % kQStages;
+        if (rb >= kQStages) mbar_wait_idle(&q_free[st], (rb / kQStages - 1) & 1, status);
+        mbar_expect_tx(&q_bar[st], kBoxes * tok * dm.G * 128);
+#pragma unroll
+        for (int x = 0; x < kBoxes; ++x) tma_load_3d(Qs + st * kTB + x * kHalfBytes, &tmQ, 64 * x, h * dm.G, s.t0 + (rb0 + rb) * tok, &q_bar[st]);
+      }
+    }
+  } else if (warp == 18) {
+    // =============================== the rows' statistics (the warp) ===============================
+    for (int rb = 0; rb < blocks; ++rb) {
+      const int ss = rb % kStatStages;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = lane + 32 * e, t = (rb0 + rb) * tok + r / dm.G;
+        v[e] = r < tok * dm.G && t < s.m ? -lse2[(size_t)(s.t0 + t) * dm.Hq + h * dm.G + r % dm.G] : -INFINITY;
+      }
+      if (rb >= kStatStages) mbar_wait_idle(&st_free[ss], (rb / kStatStages - 1) & 1, status);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) Ss[ss * kTile + lane + 32 * e] = v[e];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&st_bar[ss]);
+    }
+  } else if (warp == 16) {
+    // =============================== products (one lane) ===============================
+    if (ptx::elect_one()) {
+      constexpr uint32_t kIdesc = instr_desc_n(false, kTile);
+      const uint64_t kd0 = smem_desc(smem_u32(Ks), 16, 1024);
+      mbar_wait_idle(k_bar, 0, status);
+      for (int rb = 0; rb < blocks; ++rb) {
+        const int buf = rb & 1, st = rb % kQStages;
+        mbar_wait_idle(&q_bar[st], (rb / kQStages) & 1, status);
+        if (rb >= 2) mbar_wait_idle(&s_free[buf], ((rb - 2) >> 1) & 1, status);
+        tc_fence_after();
+        const uint64_t qd0 = smem_desc(smem_u32(Qs + st * kTB), 16, 1024);
+        for (int kk = 0; kk < tiles; ++kk) {
+#pragma unroll
+          for (int ks = 0; ks < kSteps; ++ks)
+            umma(tmem + kk * 256 + buf * 128, kd0 + (uint64_t)((kk * kTB) >> 4) + k_major_step(ks), qd0 + k_major_step(ks), kIdesc, ks > 0);
+        }
+        if (rb + kQStages < blocks) umma_commit(&q_free[st]);
+        umma_commit(&s_bar[buf]);
+      }
+    }
+  } else {
+    // =============================== two threads per key ===============================
+    const float scale2 = dm.scale * kLog2e;
+    const int kk = (warp >> 2) & 1, rh = warp >> 3, key = tid & (kKeys - 1), j = j0 + key;
+    const int need = (j - first) * dm.G;  // the first of the pair's rows that sees the key
+    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kk * 256 + rh * 64;
+    float total = 0.f, low = 0.f;  // the sum over row blocks, and what its additions lost
+    for (int rb = 0; rb < blocks; ++rb) {
+      const int buf = rb & 1, ss = rb % kStatStages, r0 = (rb0 + rb) * tok * dm.G + rh * 64;
+      // rows of the block that see the key; masked: not all of them for all keys of this CTA
+      const int lo = need - r0, hi = min(tok, s.m - (rb0 + rb) * tok) * dm.G - rh * 64;
+      const bool masked = (rb0 + rb) * tok < j0 + kKeys - 1 - first || hi < 64;
+      mbar_wait(&s_bar[buf], (rb >> 1) & 1, status);
+      mbar_wait(&st_bar[ss], (rb / kStatStages) & 1, status);
+      tc_fence_after();
+      float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      uint32_t va[16], vb[16];
+      float4 sa[4], sb[4];
+      const float* stat = Ss + ss * kTile + rh * 64;
+      // two register sets take turns: the next 16 rows' logits and statistics are on their way while these are summed
+      tmem_ld16_issue(t_lane + buf * 128, va);
+      lds16_issue(stat, sa);
+      tmem_ld16_wait(va);
+      tmem_ld16_issue(t_lane + buf * 128 + 16, vb);
+      lds16_issue(stat + 16, sb);
+      add_weights(va, sa, scale2, masked, lo, hi, acc);
+      tmem_ld16_wait(vb);
+      tmem_ld16_issue(t_lane + buf * 128 + 32, va);
+      lds16_issue(stat + 32, sa);
+      add_weights(vb, sb, scale2, masked, lo - 16, hi - 16, acc);
+      tmem_ld16_wait(va);
+      tmem_ld16_issue(t_lane + buf * 128 + 48, vb);
+      lds16_issue(stat + 48, sb);
+      add_weights(va, sa, scale2, masked, lo - 32, hi - 32, acc);
+      tmem_ld16_wait(vb);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_free[buf]);
+      add_weights(vb, sb, scale2, masked, lo - 48, hi - 48, acc);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&st_free[ss]);
+      const float x = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) - low;
+      const float t = total + x;
+      low = (t - total) - x;
+      total = t;
+    }
+    if (rh == 1) half[key] = total;
+    asm volatile("bar.sync 1, %0;" ::"n"(kKeyThreads) : "memory");
+    if (rh == 0 && j < s.n) {
+      total += half[key];
+      if (kPaged) mass[pool_row(dm, sq, b, h, j, status)] += total;
+      else mass[(size_t)(s.t0 + j) * dm.Hkv + h] = total;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace tcore
+}  // namespace paged
+}  // namespace caote

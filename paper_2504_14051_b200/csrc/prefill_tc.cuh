@@ -785,27 +785,6 @@ inline size_t score_smem_bytes() {
   return 1024 + (4 + kQStages) * (size_t)kTileBytesOf<D> + (kSStages * 2 * kTile + 2 * (D + 4) + 6 * kScoreKeys) * sizeof(float) + 320;
 }
 
-// 2^x for two arguments at once on the FMA pipe instead of the special-function unit: x = i + f with i the nearest
-// integer (taken from the low bits of x + 1.5 * 2^23), 2^f on [-1/2, 1/2] by a polynomial of degree 4 that is exact at
-// f = 0 (relative error below 3e-6), and i added to the exponent field. Arguments below -126 give about 2^-126.
-// The score pass is bound by the special-function unit's 16 results per clock and SM (one exponential per
-// (row, key) pair); it hands a quarter of them to this routine.
-__device__ __forceinline__ float2 poly_exp2x2(float2 x) {
-  constexpr float kMagic = 12582912.f;
-  x.x = fmaxf(x.x, -126.f);
-  x.y = fmaxf(x.y, -126.f);
-  const float2 t = __fadd2_rn(x, make_float2(kMagic, kMagic));
-  const float2 r = __fadd2_rn(t, make_float2(-kMagic, -kMagic));
-  const float2 f = __ffma2_rn(r, make_float2(-1.f, -1.f), x);
-  float2 p = __ffma2_rn(make_float2(0.009589649736881256f, 0.009589649736881256f), f,
-                        make_float2(0.05590599775314331f, 0.05590599775314331f));
-  p = __ffma2_rn(p, f, make_float2(0.24023915827274323f, 0.24023915827274323f));
-  p = __ffma2_rn(p, f, make_float2(0.6931241154670715f, 0.6931241154670715f));
-  p = __ffma2_rn(p, f, make_float2(1.f, 1.f));
-  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
-}
-
 // Adds to a key's running sum the attention weights 2^(s * scale2 + statistic) of 16 rows (v: the logits of the
 // key against these rows, st: the rows' statistics). plain: no row is masked. Of every eight exponentials six go to
 // the special-function unit and two to the polynomial.
