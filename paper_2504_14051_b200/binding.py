@@ -348,105 +348,153 @@ def alloc_paged_workspace(p: PagedParams, device) -> torch.Tensor:
 _IO = {BF16: torch.bfloat16, F32: torch.float32}
 
 
-# What the library cannot see behind a bare address: a tensor's type, shape, layout and device.
-def _dense(fn, name, t, dtype, shape):
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{fn}: {name} has to be a contiguous {dtype} tensor of shape {tuple(shape)}, "
-                         f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+# What the library cannot see behind a bare address: a tensor's type, size, layout and device. The calls below look for
+# themselves, in one expression and without a call per tensor (11 tensors: 3 us; a loop over their descriptions: 8 us, as
+# long as the smallest calls take the GPU), and say what was wrong only when something was.
+def _refuse(fn, workspace, io, rows, f32, i32):
+    """The message for whatever is wrong: groups of {name: (tensor or None, elements)} by type; rows may be packed."""
+    here = torch._C._cuda_getDevice()
+    if workspace.get_device() != here:
+        raise ValueError(f"{fn}: the workspace has to be on the current CUDA device, it is on {workspace.device}")
+    for dtype, group in ((io, rows), (torch.float32, f32), (torch.int32, i32)):
+        for name, (t, n) in group.items():
+            if t is None:
+                continue
+            if t.get_device() != here:
+                raise ValueError(f"{fn}: {name} has to be on the current CUDA device, it is on {t.device}")
+            if t.dtype is not dtype or t.numel() != n or (dtype is not io and not t.is_contiguous()):
+                raise ValueError(f"{fn}: {name} has to be a contiguous {dtype} tensor of {n} elements, "
+                                 f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    raise ValueError(f"{fn}: pools and outputs have to be contiguous")
 
 
-def _packed(fn, name, t, dtype, shape):
-    """The token stride of a [T, heads, d] tensor that may be a slice of a wider one."""
+def _token_stride(fn, name, t):
+    """Elements from one token to the next of a [T, heads, d] tensor that may be a slice of a wider one."""
+    T, heads, d = t.shape if t.dim() == 3 else (0, 0, 0)
     s = t.stride()
-    if t.dtype is not dtype or t.shape != shape or s[2] != 1 or (s[1] != shape[2] and shape[1] != 1) or (s[0] <= 0 and shape[0] > 1):
-        raise ValueError(f"{fn}: {name} has to be a {dtype} tensor of shape {shape} with dense rows, "
-                         f"not {t.dtype} {tuple(t.shape)} with strides {s}")
-    return s[0] if shape[0] > 1 else 0
+    if T < 1 or s[2] != 1 or (s[1] != d and heads != 1) or (s[0] <= 0 and T > 1):
+        raise ValueError(f"{fn}: {name} needs dense rows [T, heads, d], its shape is {tuple(t.shape)} with strides {s}")
+    return s[0] if T > 1 else heads * d
 
 
-def _here(fn, *tensors):
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch._C._cuda_getDevice()):
-            raise ValueError(f"{fn}: every tensor has to be on the current CUDA device, one is on {t.device}")
+def _pair_stride(fn, k, v):
+    """The same for k and v, which have one stride between them."""
+    s = _token_stride(fn, "k", k)
+    if _token_stride(fn, "v", v) != s:
+        raise ValueError(f"{fn}: k and v need the same token stride")
+    return s
 
 
 def caote_prompt_attend(p, q, k, v, cu, o, lse, mass, workspace, stream=None):
     """Causal attention inside packed prompts. lse [T, Hq], mass [T, Hkv]: None if not wanted."""
-    fn, io = "caote_prompt_attend", _IO.get(p.dtype)
-    T, Hq, Hkv, d = p.total_new, p.n_q_heads, p.n_kv_heads, p.head_dim
-    _here(fn, q, k, v, cu, o, lse, mass, workspace)
-    qs, ks = _packed(fn, "q", q, io, (T, Hq, d)), _packed(fn, "k", k, io, (T, Hkv, d))
-    if _packed(fn, "v", v, io, (T, Hkv, d)) != ks:
-        raise ValueError(f"{fn}: k and v need the same token stride")
-    _dense(fn, "cu", cu, torch.int32, (p.batch + 1,))
-    _dense(fn, "o", o, io, (T, Hq, d))
-    if lse is not None:
-        _dense(fn, "lse", lse, torch.float32, (T, Hq))
-    if mass is not None:
-        _dense(fn, "mass", mass, torch.float32, (T, Hkv))
-    _check(fn, _fn.caote_prompt_attend(ctypes.byref(p), _p(q), qs, _p(k), _p(v), ks, _p(cu), _p(o), _p(lse), _p(mass),
-                                       _p(workspace), workspace.numel(), _stream(stream)))
-
-
-def _pools(fn, p, K, V, mass, pos, page_table, lens):
-    shape = (p.n_pages, p.n_kv_heads, p.page_size)
-    io = _IO.get(p.dtype)
-    _dense(fn, "K", K, io, shape + (p.head_dim,))
-    _dense(fn, "V", V, io, shape + (p.head_dim,))
-    if mass is not None:
-        _dense(fn, "mass", mass, torch.float32, shape)
-    if pos is not None:
-        _dense(fn, "pos", pos, torch.int32, shape)
-    _dense(fn, "page_table", page_table, torch.int32, (p.batch, p.max_pages))
-    _dense(fn, "lens", lens, torch.int32, (p.batch,))
+    fn, io, f32, here = "caote_prompt_attend", _IO.get(p.dtype), torch.float32, torch._C._cuda_getDevice()
+    nq, nk = p.total_new * p.n_q_heads, p.total_new * p.n_kv_heads
+    d, B1 = p.head_dim, p.batch + 1
+    if not (workspace.get_device() == here
+            and q.dtype is io and q.numel() == nq * d and q.get_device() == here
+            and k.dtype is io and k.numel() == nk * d and k.get_device() == here
+            and v.dtype is io and v.numel() == nk * d and v.get_device() == here
+            and o.dtype is io and o.numel() == nq * d and o.get_device() == here and o.is_contiguous()
+            and cu.dtype is torch.int32 and cu.numel() == B1 and cu.get_device() == here and cu.is_contiguous()
+            and (lse is None or (lse.dtype is f32 and lse.numel() == nq and lse.get_device() == here and lse.is_contiguous()))
+            and (mass is None or (mass.dtype is f32 and mass.numel() == nk and mass.get_device() == here
+                                  and mass.is_contiguous()))):
+        _refuse(fn, workspace, io, {"q": (q, nq * d), "k": (k, nk * d), "v": (v, nk * d), "o": (o, nq * d)},
+                {"lse": (lse, nq), "mass": (mass, nk)}, {"cu": (cu, B1)})
+    qs = 0 if q.is_contiguous() else _token_stride(fn, "q", q)
+    ks = 0 if k.is_contiguous() and v.is_contiguous() else _pair_stride(fn, k, v)
+    _check(fn, _fn.caote_prompt_attend(ctypes.byref(p), q.data_ptr(), qs, k.data_ptr(), v.data_ptr(), ks, cu.data_ptr(),
+                                       o.data_ptr(), None if lse is None else lse.data_ptr(),
+                                       None if mass is None else mass.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                       _stream(stream)))
 
 
 def caote_paged_append(p, K, V, mass, pos, page_table, lens, n_seen, k_new, v_new, mass_new, cu, workspace, stream=None):
     """New rows, their positions and their first weights (mass_new [T, Hkv], None: 0) into the pages."""
-    fn, io = "caote_paged_append", _IO.get(p.dtype)
-    T, Hkv, d = p.total_new, p.n_kv_heads, p.head_dim
-    _here(fn, K, V, mass, pos, page_table, lens, n_seen, k_new, v_new, mass_new, cu, workspace)
-    _pools(fn, p, K, V, mass, pos, page_table, lens)
-    ks = _packed(fn, "k_new", k_new, io, (T, Hkv, d))
-    if _packed(fn, "v_new", v_new, io, (T, Hkv, d)) != ks:
-        raise ValueError(f"{fn}: k_new and v_new need the same token stride")
-    if n_seen is not None:
-        _dense(fn, "n_seen", n_seen, torch.int32, (p.batch,))
-    if mass_new is not None:
-        _dense(fn, "mass_new", mass_new, torch.float32, (T, Hkv))
-    _dense(fn, "cu", cu, torch.int32, (p.batch + 1,))
-    _check(fn, _fn.caote_paged_append(ctypes.byref(p), _p(K), _p(V), _p(mass), _p(pos), _p(page_table), _p(lens), _p(n_seen),
-                                      _p(k_new), _p(v_new), ks, _p(mass_new), _p(cu), _p(workspace), workspace.numel(),
-                                      _stream(stream)))
+    fn, io, f32, i32 = "caote_paged_append", _IO.get(p.dtype), torch.float32, torch.int32
+    here, B, d = torch._C._cuda_getDevice(), p.batch, p.head_dim
+    nk, slots, npt = p.total_new * p.n_kv_heads, p.n_pages * p.n_kv_heads * p.page_size, B * p.max_pages
+    if not (workspace.get_device() == here
+            and K.dtype is io and K.numel() == slots * d and K.get_device() == here and K.is_contiguous()
+            and V.dtype is io and V.numel() == slots * d and V.get_device() == here and V.is_contiguous()
+            and (mass is None or (mass.dtype is f32 and mass.numel() == slots and mass.get_device() == here
+                                  and mass.is_contiguous()))
+            and (pos is None or (pos.dtype is i32 and pos.numel() == slots and pos.get_device() == here and pos.is_contiguous()))
+            and page_table.dtype is i32 and page_table.numel() == npt and page_table.get_device() == here
+            and page_table.is_contiguous()
+            and lens.dtype is i32 and lens.numel() == B and lens.get_device() == here and lens.is_contiguous()
+            and (n_seen is None or (n_seen.dtype is i32 and n_seen.numel() == B and n_seen.get_device() == here
+                                    and n_seen.is_contiguous()))
+            and k_new.dtype is io and k_new.numel() == nk * d and k_new.get_device() == here
+            and v_new.dtype is io and v_new.numel() == nk * d and v_new.get_device() == here
+            and (mass_new is None or (mass_new.dtype is f32 and mass_new.numel() == nk and mass_new.get_device() == here
+                                      and mass_new.is_contiguous()))
+            and cu.dtype is i32 and cu.numel() == B + 1 and cu.get_device() == here and cu.is_contiguous()):
+        _refuse(fn, workspace, io, {"K": (K, slots * d), "V": (V, slots * d), "k_new": (k_new, nk * d), "v_new": (v_new, nk * d)},
+                {"mass": (mass, slots), "mass_new": (mass_new, nk)},
+                {"pos": (pos, slots), "page_table": (page_table, npt), "lens": (lens, B), "n_seen": (n_seen, B), "cu": (cu, B + 1)})
+    ks = 0 if k_new.is_contiguous() and v_new.is_contiguous() else _pair_stride(fn, k_new, v_new)
+    _check(fn, _fn.caote_paged_append(ctypes.byref(p), K.data_ptr(), V.data_ptr(), None if mass is None else mass.data_ptr(),
+                                      None if pos is None else pos.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
+                                      None if n_seen is None else n_seen.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ks,
+                                      None if mass_new is None else mass_new.data_ptr(), cu.data_ptr(), workspace.data_ptr(),
+                                      workspace.numel(), _stream(stream)))
 
 
 def caote_paged_attend(p, q, K, V, mass, page_table, lens, cu, o, lse, workspace, stream=None):
     """Attention of the new tokens, the last ones of their sequences' pages. mass (None: not wanted) is added to."""
-    fn, io = "caote_paged_attend", _IO.get(p.dtype)
-    T, Hq, d = p.total_new, p.n_q_heads, p.head_dim
-    _here(fn, q, K, V, mass, page_table, lens, cu, o, lse, workspace)
-    qs = _packed(fn, "q", q, io, (T, Hq, d))
-    _pools(fn, p, K, V, mass, None, page_table, lens)
-    _dense(fn, "cu", cu, torch.int32, (p.batch + 1,))
-    _dense(fn, "o", o, io, (T, Hq, d))
-    if lse is not None:
-        _dense(fn, "lse", lse, torch.float32, (T, Hq))
-    _check(fn, _fn.caote_paged_attend(ctypes.byref(p), _p(q), qs, _p(K), _p(V), _p(mass), _p(page_table), _p(lens), _p(cu),
-                                      _p(o), _p(lse), _p(workspace), workspace.numel(), _stream(stream)))
+    fn, io, f32, i32 = "caote_paged_attend", _IO.get(p.dtype), torch.float32, torch.int32
+    here, B, d = torch._C._cuda_getDevice(), p.batch, p.head_dim
+    nq, slots, npt = p.total_new * p.n_q_heads, p.n_pages * p.n_kv_heads * p.page_size, B * p.max_pages
+    if not (workspace.get_device() == here
+            and q.dtype is io and q.numel() == nq * d and q.get_device() == here
+            and K.dtype is io and K.numel() == slots * d and K.get_device() == here and K.is_contiguous()
+            and V.dtype is io and V.numel() == slots * d and V.get_device() == here and V.is_contiguous()
+            and (mass is None or (mass.dtype is f32 and mass.numel() == slots and mass.get_device() == here
+                                  and mass.is_contiguous()))
+            and page_table.dtype is i32 and page_table.numel() == npt and page_table.get_device() == here
+            and page_table.is_contiguous()
+            and lens.dtype is i32 and lens.numel() == B and lens.get_device() == here and lens.is_contiguous()
+            and cu.dtype is i32 and cu.numel() == B + 1 and cu.get_device() == here and cu.is_contiguous()
+            and o.dtype is io and o.numel() == nq * d and o.get_device() == here and o.is_contiguous()
+            and (lse is None or (lse.dtype is f32 and lse.numel() == nq and lse.get_device() == here and lse.is_contiguous()))):
+        _refuse(fn, workspace, io, {"q": (q, nq * d), "K": (K, slots * d), "V": (V, slots * d), "o": (o, nq * d)},
+                {"mass": (mass, slots), "lse": (lse, nq)},
+                {"page_table": (page_table, npt), "lens": (lens, B), "cu": (cu, B + 1)})
+    qs = 0 if q.is_contiguous() else _token_stride(fn, "q", q)
+    _check(fn, _fn.caote_paged_attend(ctypes.byref(p), q.data_ptr(), qs, K.data_ptr(), V.data_ptr(),
+                                      None if mass is None else mass.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
+                                      cu.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(),
+                                      workspace.data_ptr(), workspace.numel(), _stream(stream)))
 
 
 def caote_paged_evict(p, K, V, mass, pos, page_table, lens, n_seen, budget, sinks, recent, evict_idx, n_evict, workspace,
                       stream=None):
     """The lightest tokens beyond the budget leave the pages; the first `sinks` and the `recent` newest go last."""
-    fn = "caote_paged_evict"
-    _here(fn, K, V, mass, pos, page_table, lens, n_seen, budget, evict_idx, n_evict, workspace)
-    _pools(fn, p, K, V, mass, pos, page_table, lens)
-    for name, t in (("n_seen", n_seen), ("budget", budget), ("n_evict", n_evict)):
-        _dense(fn, name, t, torch.int32, (p.batch,))
-    _dense(fn, "evict_idx", evict_idx, torch.int32, (p.batch, p.n_kv_heads, evict_idx.shape[-1]))
-    _check(fn, _fn.caote_paged_evict(ctypes.byref(p), _p(K), _p(V), _p(mass), _p(pos), _p(page_table), _p(lens), _p(n_seen),
-                                     _p(budget), sinks, recent, _p(evict_idx), evict_idx.shape[-1], _p(n_evict),
-                                     _p(workspace), workspace.numel(), _stream(stream)))
+    fn, io, f32, i32 = "caote_paged_evict", _IO.get(p.dtype), torch.float32, torch.int32
+    here, B, Hkv = torch._C._cuda_getDevice(), p.batch, p.n_kv_heads
+    slots, npt, most = p.n_pages * Hkv * p.page_size, B * p.max_pages, evict_idx.shape[-1]
+    rows, picks = slots * p.head_dim, B * Hkv * most
+    if not (workspace.get_device() == here
+            and K.dtype is io and K.numel() == rows and K.get_device() == here and K.is_contiguous()
+            and V.dtype is io and V.numel() == rows and V.get_device() == here and V.is_contiguous()
+            and mass.dtype is f32 and mass.numel() == slots and mass.get_device() == here and mass.is_contiguous()
+            and pos.dtype is i32 and pos.numel() == slots and pos.get_device() == here and pos.is_contiguous()
+            and page_table.dtype is i32 and page_table.numel() == npt and page_table.get_device() == here
+            and page_table.is_contiguous()
+            and lens.dtype is i32 and lens.numel() == B and lens.get_device() == here and lens.is_contiguous()
+            and n_seen.dtype is i32 and n_seen.numel() == B and n_seen.get_device() == here and n_seen.is_contiguous()
+            and budget.dtype is i32 and budget.numel() == B and budget.get_device() == here and budget.is_contiguous()
+            and evict_idx.dtype is i32 and evict_idx.numel() == picks and evict_idx.get_device() == here
+            and evict_idx.is_contiguous()
+            and n_evict.dtype is i32 and n_evict.numel() == B and n_evict.get_device() == here and n_evict.is_contiguous()):
+        _refuse(fn, workspace, io, {"K": (K, rows), "V": (V, rows)}, {"mass": (mass, slots)},
+                {"pos": (pos, slots), "page_table": (page_table, npt), "lens": (lens, B), "n_seen": (n_seen, B),
+                 "budget": (budget, B), "evict_idx": (evict_idx, picks), "n_evict": (n_evict, B)})
+    _check(fn, _fn.caote_paged_evict(ctypes.byref(p), K.data_ptr(), V.data_ptr(), mass.data_ptr(), pos.data_ptr(),
+                                     page_table.data_ptr(), lens.data_ptr(), n_seen.data_ptr(), budget.data_ptr(), sinks, recent,
+                                     evict_idx.data_ptr(), most, n_evict.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                     _stream(stream)))
 
 
 def caote_read_status(workspace, stream=None) -> int:

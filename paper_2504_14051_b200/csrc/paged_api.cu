@@ -5,6 +5,7 @@
 
 #include "launch.cuh"
 #include "paged_common.cuh"
+#include "paged_decode.cuh"
 #include "paged_evict.cuh"
 #include "paged_generic.cuh"
 #include "paged_tc.cuh"
@@ -56,10 +57,12 @@ static PDims make_dims(const caote_paged_params_t* p, bool pages, int64_t q_stri
 }
 
 // ---- workspace ------------------------------------------------------------------------------------
+// One or the other, never both in one call:
 struct Scratch {
   float* lse2;   // [T, Hq] log2-domain log-sum-exp of every row
   float* lpart;  // [splits, T, Hq] and
   float* opart;  // [splits, T, Hq, D]: what the splits of the keys contribute
+  few::Records rec;
 };
 constexpr int kMostSplits = 16;
 // Splits are only made where the row blocks of a call leave room (two CTAs of 64 rows per SM, or one of 256), so splits x rows
@@ -68,7 +71,15 @@ static long long split_rows(const PDims& dm) {
   const long long rows = (long long)dm.T * dm.Hq, most = 256LL * g_sm_count;
   return rows * kMostSplits < most ? rows * kMostSplits : most;
 }
-static size_t carve(const PDims& dm, char* base, Scratch* out) {
+// Calls with few rows per sequence over pages take the kernels of paged_decode.cuh: up to kFewRows rows of a pair. Single tokens of
+// groups up to 16, or a few drafted tokens of small groups; beyond that the row blocks' padding costs less than more columns would.
+constexpr int kFewRows = 16;
+static bool few_rows(const PDims& dm, int dtype) {
+  const long long tiles = (((long long)dm.max_pages << dm.page_shift) + few::kTok - 1) / few::kTok * dm.B * dm.Hkv;
+  return dtype == CAOTE_BF16 && dm.max_pages > 0 && dm.scale > 0.f && (long long)dm.max_new * dm.G <= kFewRows && tiles < (1LL << 31);
+}
+static int few_workers() { return g_sm_count * few::kWarps; }
+static size_t carve(const PDims& dm, int dtype, char* base, Scratch* out) {
   size_t off = 0;
   auto take = [&](size_t floats) {
     float* p = reinterpret_cast<float*>(base + off);
@@ -79,12 +90,25 @@ static size_t carve(const PDims& dm, char* base, Scratch* out) {
   s.lse2 = take((size_t)dm.T * dm.Hq);
   s.lpart = take((size_t)split_rows(dm));
   s.opart = take((size_t)split_rows(dm) * dm.D);
+  size_t most = off;
+  if (dtype == CAOTE_BF16 && dm.max_pages > 0) {
+    // (a workspace for more rows per sequence serves calls with fewer: sized for the most rows that come here)
+    off = 0;
+    const long long r = (long long)dm.max_new * dm.G;
+    const size_t rows = r > 8 ? kFewRows : 8, pairs = (size_t)dm.B * dm.Hkv;
+    s.rec.slots = dm.max_pages << dm.page_shift;
+    s.rec.plan = reinterpret_cast<int*>(take((size_t)dm.B + 2));
+    s.rec.stat = take((pairs + few_workers()) * rows);
+    s.rec.o = take((pairs + few_workers()) * rows * dm.D);
+    s.rec.logits = take(pairs * s.rec.slots * rows);
+    if (off > most) most = off;
+  }
   if (out) *out = s;
-  return off;
+  return most;
 }
 static size_t workspace_bytes(const caote_paged_params_t* p) {
   refresh_sm_count();
-  return kHeaderBytes + carve(make_dims(p, p->page_size > 0, 0, 0), nullptr, nullptr);
+  return kHeaderBytes + carve(make_dims(p, p->page_size > 0, 0, 0), p->dtype, nullptr, nullptr);
 }
 static bool workspace_ok(const void* workspace, size_t have, size_t need) { return workspace && have >= need && aligned(workspace, 256); }
 
@@ -93,7 +117,7 @@ template <typename T, int D, bool kPaged>
 static int attend_generic(const PDims& dm, const Seqs& sq, const void* q, const void* K, const void* V, void* o, float* lse, float* mass,
                           char* ws, cudaStream_t st) {
   Scratch sc;
-  carve(dm, ws + kHeaderBytes, &sc);
+  carve(dm, std::is_same<T, float>::value ? CAOTE_F32 : CAOTE_BF16, ws + kHeaderBytes, &sc);
   int* status = reinterpret_cast<int*>(ws);
   auto run = [&](auto rpt) -> int {
     constexpr int RPT = decltype(rpt)::value, kRows = generic::kRows<RPT>;
@@ -163,7 +187,7 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
     return CAOTE_ERR_CUDA;
   }
   Scratch sc;
-  carve(dm, ws + kHeaderBytes, &sc);
+  carve(dm, CAOTE_BF16, ws + kHeaderBytes, &sc);
   int* status = reinterpret_cast<int*>(ws);
   const int box = kPaged && dm.page_shift < 7 ? 1 << dm.page_shift : tcore::kTile;
   CUtensorMap tmQ, tmK, tmV;
@@ -196,12 +220,45 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
   return CAOTE_OK;
 }
 
+template <int D, int NT>
+static int attend_few(const PDims& dm, const Seqs& sq, const void* q, const void* K, const void* V, void* o, float* lse, float* mass, char* ws,
+                      cudaStream_t st) {
+  if (!tensor_map_encoder()) {
+    snprintf(g_cuda_error, sizeof(g_cuda_error), "cuTensorMapEncodeTiled is not to be had");
+    return CAOTE_ERR_CUDA;
+  }
+  Scratch sc;
+  carve(dm, CAOTE_BF16, ws + kHeaderBytes, &sc);
+  if (!mass) sc.rec.logits = nullptr;
+  int* status = reinterpret_cast<int*>(ws);
+  CUtensorMap tmK, tmV;
+  int rc = encode_keys(dm, K, true, few::kTok, &tmK);
+  if (!rc) rc = encode_keys(dm, V, true, few::kTok, &tmV);
+  if (!rc) rc = allow_smem(few::decode_kernel<D, NT>, few::decode_smem<D>());
+  if (rc) return rc;
+  CAOTE_LAUNCH("paged_decode_kernel", st,
+               launch_pdl(few::decode_kernel<D, NT>, dim3(g_sm_count), dim3(few::kThreads), few::decode_smem<D>(), st, tmK, tmV, dm, sq,
+                          (const __nv_bfloat16*)q, sc.rec, status));
+  const int chunks = mass ? (sc.rec.slots + few::kChunk - 1) / few::kChunk : 1;
+  CAOTE_LAUNCH("paged_finish_kernel", st,
+               launch_pdl(few::finish_kernel<D, NT>, dim3(chunks, dm.B * dm.Hkv), dim3(256), 0, st, dm, sq, sc.rec, (__nv_bfloat16*)o, lse, mass,
+                          status));
+  return CAOTE_OK;
+}
+
 template <bool kPaged>
 static int attend(const caote_paged_params_t* p, const PDims& dm, const Seqs& sq, const void* q, const void* K, const void* V, void* o,
                   float* lse, float* mass, char* ws, cudaStream_t st) {
   if (p->dtype == CAOTE_F32)
     return dm.D == 128 ? attend_generic<float, 128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st)
                        : attend_generic<float, 64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
+  if constexpr (kPaged) {
+    if (few_rows(dm, p->dtype) && dm.B * dm.Hkv <= 65535) {
+      const bool one = dm.max_new * dm.G <= 8;
+      if (dm.D == 128) return one ? attend_few<128, 1>(dm, sq, q, K, V, o, lse, mass, ws, st) : attend_few<128, 2>(dm, sq, q, K, V, o, lse, mass, ws, st);
+      return one ? attend_few<64, 1>(dm, sq, q, K, V, o, lse, mass, ws, st) : attend_few<64, 2>(dm, sq, q, K, V, o, lse, mass, ws, st);
+    }
+  }
   if (dm.scale > 0.f)  // (the tensor-core kernels take the largest product for the largest logit)
     return dm.D == 128 ? attend_tc<128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st) : attend_tc<64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
   return dm.D == 128 ? attend_generic<__nv_bfloat16, 128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st)
@@ -229,7 +286,7 @@ int caote_prompt_attend(const caote_paged_params_t* p, const void* q, int64_t q_
   if (!paged::stride_ok(p, q_stride, p->n_q_heads) || !paged::stride_ok(p, kv_stride, p->n_kv_heads)) return CAOTE_ERR_INVALID_ARG;
   refresh_sm_count();
   const paged::PDims dm = paged::make_dims(p, false, q_stride, kv_stride);
-  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes + paged::carve(dm, nullptr, nullptr))) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes + paged::carve(dm, p->dtype, nullptr, nullptr))) return CAOTE_ERR_INVALID_ARG;
   int rc = check_device();
   if (rc) return rc;
   return paged::attend<false>(p, dm, paged::Seqs{cu, nullptr, nullptr}, q, k, v, o, lse, mass, (char*)workspace, (cudaStream_t)stream);
@@ -267,7 +324,7 @@ int caote_paged_attend(const caote_paged_params_t* p, const void* q, int64_t q_s
   if (!paged::stride_ok(p, q_stride, p->n_q_heads)) return CAOTE_ERR_INVALID_ARG;
   refresh_sm_count();
   const paged::PDims dm = paged::make_dims(p, true, q_stride, 0);
-  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes + paged::carve(dm, nullptr, nullptr))) return CAOTE_ERR_INVALID_ARG;
+  if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes + paged::carve(dm, p->dtype, nullptr, nullptr))) return CAOTE_ERR_INVALID_ARG;
   int rc = check_device();
   if (rc) return rc;
   return paged::attend<true>(p, dm, paged::Seqs{cu, len, page_table}, q, K, V, o, lse, mass, (char*)workspace, (cudaStream_t)stream);

@@ -59,14 +59,14 @@ def test_workspace_size_refuses(bad):
 def test_workspace_for_more_rows_serves_fewer():
     for dtype in (torch.bfloat16, torch.float32):
         for heads in [(4, 2), (28, 4), (64, 8)]:
-            last = 0
+            last = {}
             for T in [1, 2, 7, 16, 64, 100, 500, 2048, 16384]:
-                sizes = [C.caote_paged_workspace_bytes(params(n_q_heads=heads[0], n_kv_heads=heads[1], total_new=T, max_new=m, dtype=dtype,
-                                                              batch=64, n_pages=4000, max_pages=512))
-                         for m in [1, 2, 5, 16, 33, 512, 16384] if m <= T]
-                assert sizes == sorted(sizes) and sizes[0] >= min(last, sizes[0])
-                assert sizes[-1] >= last
-                last = sizes[-1]
+                sizes = {m: C.caote_paged_workspace_bytes(params(n_q_heads=heads[0], n_kv_heads=heads[1], total_new=T, max_new=m, dtype=dtype,
+                                                                 batch=64, n_pages=4000, max_pages=512))
+                         for m in [1, 2, 5, 16, 33, 512, 16384] if m <= T}
+                assert list(sizes.values()) == sorted(sizes.values())
+                assert all(sizes[m] >= last[m] for m in last)
+                last = sizes
 
 
 def test_refusals_come_before_any_launch():
@@ -107,7 +107,8 @@ def test_refusals_come_before_any_launch():
     for f, name, dense in [(prompt, "qs", 1024), (prompt, "ks", 256), (attend, "qs", 1024), (append, "ks", 256)]:
         for stride in (dense - 8, dense + 4, -dense, 1 << 31):
             assert f(**{name: stride}) == C.ERR_INVALID_ARG, (f, name, stride)
-    assert prompt(n=need - 1) == attend(n=need - 1) == C.ERR_INVALID_ARG
+    assert attend(n=need - 1) == C.ERR_INVALID_ARG
+    assert prompt(n=C.caote_paged_workspace_bytes(params(page_size=0, n_pages=0, max_pages=0)) - 1) == C.ERR_INVALID_ARG
     assert evict(sinks=-1) == evict(recent=-1) == evict(most=0) == C.ERR_INVALID_ARG
     assert C.caote_launch_count() == before
 
@@ -121,23 +122,54 @@ def test_calls_fail_loudly_without_a_gpu():
     assert rc in (C.ERR_CUDA, C.ERR_UNSUPPORTED)
 
 
-def test_the_binding_refuses_what_an_address_does_not_show():
-    io = torch.bfloat16
-    q, k = torch.zeros(6, 8, 128, dtype=io), torch.zeros(6, 2, 128, dtype=io)
-    with pytest.raises(ValueError, match="device"):
-        P.caote_prompt_attend(params(), q, k, k, torch.zeros(3, dtype=torch.int32), q, None, None, torch.zeros(256, dtype=torch.uint8))
-    fn = "f"
+def test_the_binding_refuses_what_an_address_does_not_show(monkeypatch):
+    """Types, sizes, layouts and devices (here everything is on the CPU, which is made to look like the current device)."""
+    calls = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: calls.append((name, a)) or 0
+
+    monkeypatch.setattr(C, "_fn", Lib())
+    monkeypatch.setattr(C, "_stream", lambda s: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)
+    io, p = torch.bfloat16, params()
+    z = {"q": torch.zeros(6, 8, 128, dtype=io), "k": torch.zeros(6, 2, 128, dtype=io), "cu": torch.zeros(3, dtype=torch.int32),
+         "lse": torch.zeros(6, 8), "mass_new": torch.zeros(6, 2), "ws": torch.zeros(256, dtype=torch.uint8),
+         "K": torch.zeros(10, 2, 16, 128, dtype=io), "mass": torch.zeros(10, 2, 16), "pos": torch.zeros(10, 2, 16, dtype=torch.int32),
+         "table": torch.zeros(2, 4, dtype=torch.int32), "b": torch.zeros(2, dtype=torch.int32),
+         "out": torch.zeros(2, 2, 5, dtype=torch.int32)}
+    forms = {
+        P.caote_prompt_attend: ["q", "k", "k", "cu", "q", "lse", "mass_new", "ws"],
+        P.caote_paged_append: ["K", "K", "mass", "pos", "table", "b", "b", "k", "k", "mass_new", "cu", "ws"],
+        P.caote_paged_attend: ["q", "K", "K", "mass", "table", "b", "cu", "q", "lse", "ws"],
+        P.caote_paged_evict: ["K", "K", "mass", "pos", "table", "b", "b", "b", 4, 64, "out", "b", "ws"]}
+    for f, names in forms.items():
+        good = [z.get(x, x) if isinstance(x, str) else x for x in names]
+        f(p, *good)
+        for i, x in enumerate(good):
+            if not isinstance(x, torch.Tensor) or names[i] == "ws":
+                continue
+            wrong = [x.double(), x[:-1].contiguous(), torch.cat([x, x])]
+            if names[i] not in ("q", "k"):
+                wrong.append(torch.stack([x, x], -1)[..., 0])
+            for bad in wrong if names[i] != "out" else wrong[:1] + wrong[3:]:
+                with pytest.raises(ValueError):
+                    f(p, *good[:i], bad, *good[i + 1:])
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+        with pytest.raises(ValueError, match="device"):
+            f(p, *good)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1)
+    assert [n for n, _ in calls] == [f.__name__ for f in forms]
     wide = torch.zeros(6, 12, 128, dtype=io)
-    assert C._packed(fn, "q", wide[:, :8], io, (6, 8, 128)) == 12 * 128
-    assert C._packed(fn, "k", k, io, (6, 2, 128)) == 256
-    assert C._packed(fn, "q", wide[:1, :8], io, (1, 8, 128)) == 0
-    for bad in (q.float(), q[:, :, :64], q.transpose(0, 1), q[:1].expand(6, 8, 128), wide[:, ::2][:, :4].expand(6, 4, 128),
-                torch.zeros(6, 8, 256, dtype=io)[:, :, ::2]):
+    P.caote_prompt_attend(p, wide[:, :8], wide[:, 8:10], wide[:, 10:], z["cu"], z["q"], None, None, z["ws"])
+    assert calls[-1][1][2] == calls[-1][1][5] == 12 * 128
+    for bad in (z["q"].transpose(0, 1).contiguous().transpose(0, 1), z["q"][:1].expand(6, 8, 128),
+                torch.zeros(6, 8, 256, dtype=io)[:, :, ::2], torch.zeros(6, 16, 128, dtype=io)[:, ::2]):
         with pytest.raises(ValueError):
-            C._packed(fn, "q", bad, io, (6, 8, 128))
-    for bad in (torch.zeros(3), torch.zeros(4, dtype=torch.int32), torch.zeros(6, dtype=torch.int32)[::2]):
-        with pytest.raises(ValueError):
-            C._dense(fn, "cu", bad, torch.int32, (3,))
+            P.caote_paged_attend(p, bad, z["K"], z["K"], None, z["table"], z["b"], z["cu"], z["q"], None, z["ws"])
+    with pytest.raises(ValueError, match="stride"):
+        P.caote_prompt_attend(p, z["q"], wide[:, 8:10], z["k"], z["cu"], z["q"], None, None, z["ws"])
 
 
 def test_page_bookkeeping_on_the_host(monkeypatch):
