@@ -59,12 +59,13 @@ static PDims make_dims(const caote_paged_params_t* p, bool pages, int64_t q_stri
 // ---- workspace ------------------------------------------------------------------------------------
 // One or the other, never both in one call:
 struct Scratch {
-  float* lse2;   // [T, Hq] log2-domain log-sum-exp of every row
+  float* lse2;   // [Hkv, T, G] log2-domain log-sum-exp of every row
   float* lpart;  // [splits, T, Hq] and
   float* opart;  // [splits, T, Hq, D]: what the splits of the keys contribute
   few::Records rec;
 };
 constexpr int kMostSplits = 16;
+constexpr int kItemCounter = 12;  // word of the workspace header
 // Splits are only made where the row blocks of a call leave room (two CTAs of 64 rows per SM, or one of 256), so splits x rows
 // stays below what these hold; a bound that grows with T and does not depend on how the rows lie.
 static long long split_rows(const PDims& dm) {
@@ -122,7 +123,7 @@ static int attend_generic(const PDims& dm, const Seqs& sq, const void* q, const 
   auto run = [&](auto rpt) -> int {
     constexpr int RPT = decltype(rpt)::value, kRows = generic::kRows<RPT>;
     const size_t smem = generic::smem_bytes<D, RPT>();
-    const long long blocks = (long long)dm.T * dm.G / kRows + dm.B;
+    const long long blocks = ((long long)dm.T * dm.G + dm.B * (kRows - 1LL)) / kRows;  // (no way to lie makes more)
     long long splits = 2LL * g_sm_count / (blocks * dm.Hkv);
     const long long tiles = kPaged ? (((long long)dm.max_pages << dm.page_shift) + generic::kKeys - 1) / generic::kKeys : 0;
     if (splits > tiles / generic::kLeastTiles) splits = tiles / generic::kLeastTiles;
@@ -198,16 +199,18 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
   if (!rc && mass) rc = allow_smem(tcore::mass_kernel<D, kPaged>, tcore::mass_smem<D>());
   if (rc) return rc;
   const int tok = tcore::kTile / dm.G;
-  const long long blocks = dm.T / (2 * tok) + dm.B, cap = (long long)dm.max_pages << dm.page_shift;
+  const long long blocks = (dm.T + dm.B * (2LL * tok - 1)) / (2 * tok), cap = (long long)dm.max_pages << dm.page_shift;
   long long splits = g_sm_count / (blocks * dm.Hkv);
   if (splits > cap / tcore::kTile / tcore::kLeastTiles) splits = cap / tcore::kTile / tcore::kLeastTiles;
   if (splits > kMostSplits) splits = kMostSplits;
   if (splits < 1) splits = 1;
-  const long long key_blocks = kPaged ? (cap + tcore::kKeys - 1) / tcore::kKeys * dm.B : (long long)dm.T / tcore::kKeys + dm.B;
-  if (blocks > 0x7fffffffLL || key_blocks > 0x7fffffffLL) return CAOTE_ERR_UNSUPPORTED;
+  // (items of the mass kernel are numbered in 32 bits)
+  const long long key_blocks = (kPaged ? (cap + tcore::kKeys - 1) / tcore::kKeys * dm.B : (long long)dm.T / tcore::kKeys + dm.B) * dm.Hkv;
+  if (blocks > 0x7fffffffLL || key_blocks > 0x7fff0000LL) return CAOTE_ERR_UNSUPPORTED;
   CAOTE_LAUNCH("paged_attend_kernel", st,
                launch_pdl(tcore::attend_kernel<D, kPaged>, dim3((unsigned)blocks, dm.Hkv, (unsigned)splits), dim3(tcore::kAttendThreads),
-                          tcore::attend_smem<D>(), st, tmQ, tmK, tmV, dm, sq, box, (__nv_bfloat16*)o, lse, sc.lse2, sc.opart, sc.lpart, status));
+                          tcore::attend_smem<D>(), st, tmQ, tmK, tmV, dm, sq, box, (__nv_bfloat16*)o, lse, sc.lse2, sc.opart, sc.lpart, status + kItemCounter,
+                          status));
   if (splits > 1)
     CAOTE_LAUNCH("paged_combine", st,
                  launch_pdl(generic::combine_kernel<__nv_bfloat16, D>, dim3((unsigned)(((long long)dm.T * dm.Hq + 7) / 8)), dim3(256), 0, st, dm,
@@ -215,8 +218,8 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
                             (__nv_bfloat16*)o, lse, sc.lse2));
   if (mass)
     CAOTE_LAUNCH("paged_mass_kernel", st,
-                 launch_pdl(tcore::mass_kernel<D, kPaged>, dim3((unsigned)key_blocks, dm.Hkv), dim3(tcore::kMassThreads), tcore::mass_smem<D>(),
-                            st, tmQ, tmK, dm, sq, box, (const float*)sc.lse2, mass, status));
+                 launch_pdl(tcore::mass_kernel<D, kPaged>, dim3(g_sm_count), dim3(tcore::kMassThreads), tcore::mass_smem<D>(), st, tmQ, tmK, dm,
+                            sq, box, (const float*)sc.lse2, mass, status + kItemCounter, status));
   return CAOTE_OK;
 }
 

@@ -47,6 +47,9 @@ __device__ __forceinline__ Seq sequence(const PDims& dm, const Seqs& sq, int b, 
   return s;
 }
 
+// Where the statistic of query row r of a pair lies in the workspace: [Hkv][T][G], so that a block of rows is contiguous.
+__device__ __forceinline__ size_t stat_at(const PDims& dm, const Seq& s, int h, int r) { return ((size_t)h * dm.T + s.t0) * dm.G + r; }
+
 // Work is numbered over all sequences: sequence b has ceil(what(b) / per) blocks. The sequence that block `index` belongs to
 // and its number in there; false: no such block. For one whole warp, the same result in all lanes.
 template <typename What>

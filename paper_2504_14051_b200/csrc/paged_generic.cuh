@@ -193,7 +193,7 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
     const float inv = l[r] > 0.f ? 1.f / l[r] : 0.f, stat = top[r] + __log2f(l[r]);  // (no key in this split: -inf)
     if (count == 1) {
       if (tx == 0) {
-        lse2[at] = stat;
+        lse2[stat_at(dm, s, h, row)] = stat;
         if (lse) lse[at] = stat * kLn2;
       }
 #pragma unroll
@@ -249,7 +249,8 @@ combine_kernel(PDims dm, Seqs sq, int splits, int keys_per_tile, int least_tiles
   for (int c = 0; c < CPL; ++c) o[at * D + c * 32 + lane] = from_float<T>(x[c] / sum);
   if (lane == 0) {
     stat += __log2f(sum);
-    lse2[at] = stat;
+    const int hq = (int)(at % dm.Hq);
+    lse2[stat_at(dm, s, hq / dm.G, (t - s.t0) * dm.G + hq % dm.G)] = stat;
     if (lse) lse[at] = stat * kLn2;
   }
 }
@@ -288,7 +289,7 @@ mass_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ K,
     load_rows<T, D, RPT>(dm, q, s, h, r0, Qs);
     if (tid < kRows<RPT>) {
       const int r = r0 + tid;
-      Ps[tid] = r < R ? lse2[(size_t)(s.t0 + r / dm.G) * dm.Hq + h * dm.G + r % dm.G] : 0.f;
+      Ps[tid] = r < R ? lse2[stat_at(dm, s, h, r)] : 0.f;
     }
     __syncthreads();
     float x[RPT][4];

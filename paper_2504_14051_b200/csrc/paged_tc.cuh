@@ -73,13 +73,13 @@ __device__ __forceinline__ void copy_keys(const PDims& dm, const CUtensorMap* tm
   __syncwarp();
 }
 
-// grid = (pairs of row blocks of all sequences, Hkv, splits). lse2 [T, Hq]: the rows' statistics for the mass; with more than one
+// grid = (pairs of row blocks of all sequences, Hkv, splits). lse2: the rows' statistics for the mass (stat_at); with more than one
 // split opart, lpart as in generic::attend_kernel.
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kAttendThreads, 1)
 attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               PDims dm, Seqs sq, int box, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ lse2,
-              float* __restrict__ opart, float* __restrict__ lpart, int* status) {
+              float* __restrict__ opart, float* __restrict__ lpart, int* next_item, int* status) {
   constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16, kKS = kKStages<D>, kVS = kVStages<D>;
   ptx::pdl_wait();
   ptx::pdl_trigger();
@@ -104,6 +104,7 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     if (lane == 0) { where[0] = b; where[1] = block; }
   } else if (warp == 1 && blockIdx.x == 0 && h == 0 && split == 0) {
     for (int x = lane; x < dm.B; x += 32) sequence(dm, sq, x, status);
+    if (lane == 0) *next_item = 0;  // (for the mass kernel)
   }
   if (tid == 0) {
     for (int i = 0; i < kBars1; ++i) mbar_init(&bars[i], 1);
@@ -300,7 +301,7 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const size_t at = (size_t)(s.t0 + tkn) * dm.Hq + h * dm.G + row % dm.G;
     if (count == 1) {
       if (valid) {
-        lse2[at] = stat;
+        lse2[stat_at(dm, s, h, (i0 + i * tok) * dm.G + row)] = stat;
         if (lse) lse[at] = stat * kLn2;
       }
 #pragma unroll
@@ -337,22 +338,27 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 }
 
 // ---- the weight that every key received ------------------------------------------------------------------
-constexpr int kKeys = 2 * kTile;                       // keys per CTA
+// Persistent: a CTA takes items of 256 keys from a counter, the next item's K on its way while this one's rows go by. The warps
+// that copy and issue run ahead of the key threads across items; rows, statistics and S buffers are counted through.
+constexpr int kKeys = 2 * kTile;                       // keys per item
 constexpr int kKeyThreads = 2 * kKeys;                 // two threads per key: 64 rows of a row block each
-constexpr int kMassThreads = kKeyThreads + 96;         // + products, K and Q copies, statistics
-constexpr int kQStages = 3, kStatStages = 4;
+constexpr int kMassThreads = kKeyThreads + 128;        // + products, items and K, Q, statistics
+constexpr int kStatStages = 4;
 template <int D>
-constexpr size_t mass_smem() { return 1024 + (size_t)(2 + kQStages) * kTileBytesOf<D> + (kStatStages * kTile + kKeys) * sizeof(float) + 512; }
+constexpr int kQStages = D == 128 ? 2 : 4;
+template <int D>
+constexpr size_t mass_smem() { return 1024 + (size_t)(4 + kQStages<D>) * kTileBytesOf<D> + (kStatStages * kTile + 2 * kKeys) * sizeof(float) + 512; }
 
-// Adds the weights 2^(s * scale2 + stat) of a key in 16 rows to acc; two of eight exponentials on the FMA pipe. masked: only rows
+// Adds the weights 2^(s * scale2 + stat) of a key in 16 rows to acc; two of eight exponentials on the FMA pipe. kMasked: only rows
 // [lo, hi) of them count (the others' products may be anything).
-__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], const float4 (&st)[4], float scale2, bool masked, int lo, int hi, float2 (&acc)[2]) {
+template <bool kMasked>
+__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], const float4 (&st)[4], float scale2, int lo, int hi, float2 (&acc)[2]) {
   const float2 scale22 = make_float2(scale2, scale2);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1])), scale22, make_float2(st[k].x, st[k].y));
     float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3])), scale22, make_float2(st[k].z, st[k].w));
-    if (masked) {
+    if (kMasked) {
       if (4 * k < lo || 4 * k >= hi) a.x = -INFINITY;
       if (4 * k + 1 < lo || 4 * k + 1 >= hi) a.y = -INFINITY;
       if (4 * k + 2 < lo || 4 * k + 2 >= hi) b.x = -INFINITY;
@@ -365,159 +371,256 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[16], const float
   }
 }
 
-// grid = (blocks of 256 keys of all sequences, Hkv).
+struct Item {
+  int b, h, j0, rb0, blocks;  // b < 0: no more; rb0: the first row block (of 128 / G tokens) that sees any of the keys
+  Seq s;
+};
+
+// grid: one CTA per SM. next_item: 0 at the start (the attention pass leaves it so).
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kMassThreads, 1)
 mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, PDims dm, Seqs sq, int box,
-            const float* __restrict__ lse2, float* __restrict__ mass, int* status) {
-  constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16;
+            const float* __restrict__ lse2, float* __restrict__ mass, int* next_item, int* status) {
+  constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16, kQS = kQStages<D>;
   ptx::pdl_wait();
   ptx::pdl_trigger();
   extern __shared__ char smem_raw[];
   char* sm = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
-  char* Ks = sm;                                                      // [2]
-  char* Qs = Ks + 2 * kTB;                                            // [kQStages]
-  float* Ss = reinterpret_cast<float*>(Qs + kQStages * kTB);          // [kStatStages][kTile] minus the rows' lse2
-  float* half = Ss + kStatStages * kTile;                             // [kKeys]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(half + kKeys);
-  uint64_t *k_bar = &bars[0], *q_bar = &bars[1], *q_free = q_bar + kQStages, *s_bar = q_free + kQStages, *st_bar = s_bar + 2,
-           *s_free = st_bar + kStatStages, *st_free = s_free + 2;
-  constexpr int kBars1 = 1 + 2 * kQStages + 2 + kStatStages;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars1 + 2 + kStatStages);
-  int* where = reinterpret_cast<int*>(tmem_slot + 1);
+  char* Ks = sm;                                              // [2][2] tiles of an item
+  char* Qs = Ks + 4 * kTB;                                    // [kQS]
+  float* Ss = reinterpret_cast<float*>(Qs + kQS * kTB);       // [kStatStages][kTile] minus the rows' lse2
+  float* half = Ss + kStatStages * kTile;                     // [2][kKeys] the upper halves' sums
+  uint64_t* bars = reinterpret_cast<uint64_t*>(half + 2 * kKeys);
+  uint64_t *k_bar = &bars[0], *q_bar = k_bar + 2, *q_free = q_bar + kQS, *s_bar = q_free + kQS, *st_bar = s_bar + 2,
+           *s_free = st_bar + kStatStages, *st_free = s_free + 2, *item_free = st_free + kStatStages;
+  constexpr int kBars1 = 2 + 2 * kQS + 2 + kStatStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_free + 2);
+  __shared__ Item items[2];
 
-  const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index(), h = blockIdx.y;
-  if (warp == 0) {
-    int b = -1, block = 0;
-    if (!locate(dm.B, kKeys, blockIdx.x, [&](int x) { const Seq s = sequence(dm, sq, x); return s.m > 0 ? s.n : 0; }, b, block)) b = -1;
-    if (lane == 0) { where[0] = b; where[1] = block; }
-  }
+  const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
   if (tid == 0) {
     for (int i = 0; i < kBars1; ++i) mbar_init(&bars[i], 1);
-    for (int i = kBars1; i < kBars1 + 2 + kStatStages; ++i) mbar_init(&bars[i], kKeyThreads / 32);
+    for (int i = 0; i < 2 + kStatStages; ++i) mbar_init(&s_free[i], kKeyThreads / 32);
+    // an item's place comes free when the key warps, the Q copies, the statistics and the products are done with it
+    for (int i = 0; i < 2; ++i) mbar_init(&item_free[i], kKeyThreads / 32 + 3);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  __syncthreads();
-  const int b = where[0], j0 = where[1] * kKeys;
-  if (b < 0) return;
-  const Seq s = sequence(dm, sq, b);
-  const int first = s.n - s.m, tok = kTile / dm.G;
-  // row blocks that see any of the keys
-  const int rb0 = max(0, j0 - first) / tok, blocks = (s.m + tok - 1) / tok - rb0;
-  const int tiles = j0 + kTile < s.n ? 2 : 1;
-
   if (warp == 0) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;  // S^T of key tile kk, buffer buf: columns [kk * 256 + buf * 128, + 128)
+  const int tok = kTile / dm.G;
 
   if (warp == 17) {
-    // =============================== copies of K and of the Q blocks ===============================
-    if (lane == 0) mbar_expect_tx(k_bar, (boxes_of<kPaged>(s, j0, box) + (tiles == 2 ? boxes_of<kPaged>(s, j0 + kTile, box) : 0)) * box * D * 2);
-    __syncwarp();
-    for (int kk = 0; kk < tiles; ++kk) {
-      const int id = page_of<kPaged>(dm, sq, b, s.n, j0 + kk * kTile, box, status);
-      copy_keys<D, kPaged>(dm, &tmK, s, h, j0 + kk * kTile, box, id, Ks + kk * kTB, k_bar);
-    }
-    if (ptx::elect_one()) {
-      for (int rb = 0; rb < blocks; ++rb) {
-        const int st = rb % kQStages;
-        if (rb >= kQStages) mbar_wait_idle(&q_free[st], (rb / kQStages - 1) & 1, status);
-        mbar_expect_tx(&q_bar[st], kBoxes * tok * dm.G * 128);
-#pragma unroll
-        for (int x = 0; x < kBoxes; ++x) tma_load_3d(Qs + st * kTB + x * kHalfBytes, &tmQ, 64 * x, h * dm.G, s.t0 + (rb0 + rb) * tok, &q_bar[st]);
+    // =============================== items and their K (the warp) ===============================
+    auto blocks_of_seq = [&](int x) { const Seq s = sequence(dm, sq, x); return s.m > 0 ? s.n : 0; };
+    for (int c = 0;; ++c) {
+      const int buf = c & 1;
+      int it = 0;
+      if (lane == 0) it = atomicAdd(next_item, 1);
+      it = __shfl_sync(0xffffffffu, it, 0);
+      Item x;
+      // A prompt's first keys are seen by most rows: the heads take turns, so that what comes last is short. (Head by head the
+      // last head's first keys come late: 2.84 instead of 1.4 ms, 64/8 heads, prompts of 7 428 and 8 956 tokens.)
+      int block = 0;
+      if (locate(dm.B, kKeys, it / dm.Hkv, blocks_of_seq, x.b, block)) {
+        x.h = it % dm.Hkv;
+        x.s = sequence(dm, sq, x.b);
+        x.j0 = block * kKeys;
+        x.rb0 = max(0, x.j0 - (x.s.n - x.s.m)) / tok;
+        x.blocks = (x.s.m + tok - 1) / tok - x.rb0;
+      } else {
+        x.b = -1;
       }
+      int id[2] = {0, 0}, boxes[2] = {0, 0};
+      if (x.b >= 0) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+          if (x.j0 + kk * kTile < x.s.n) {
+            id[kk] = page_of<kPaged>(dm, sq, x.b, x.s.n, x.j0 + kk * kTile, box, status);
+            boxes[kk] = boxes_of<kPaged>(x.s, x.j0 + kk * kTile, box);
+          }
+      }
+      if (c >= 2) mbar_wait_idle(&item_free[buf], ((c >> 1) - 1) & 1, status);
+      if (lane == 0) {
+        items[buf] = x;
+        if (x.b >= 0) mbar_expect_tx(&k_bar[buf], (boxes[0] + boxes[1]) * box * D * 2);  // (also says that the item is there)
+        else mbar_arrive(&k_bar[buf]);
+      }
+      __syncwarp();
+      if (x.b < 0) break;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        if (boxes[kk] > 0) copy_keys<D, kPaged>(dm, &tmK, x.s, x.h, x.j0 + kk * kTile, box, id[kk], Ks + (2 * buf + kk) * kTB, &k_bar[buf]);
     }
   } else if (warp == 18) {
-    // =============================== the rows' statistics (the warp) ===============================
-    for (int rb = 0; rb < blocks; ++rb) {
-      const int ss = rb % kStatStages;
-      float v[4];
+    // =============================== copies of the Q blocks (one lane) ===============================
+    if (ptx::elect_one()) {
+      int qb = 0;
+      for (int c = 0;; ++c) {
+        mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status);
+        const Item x = items[c & 1];
+        if (x.b < 0) break;
+        for (int rb = 0; rb < x.blocks; ++rb, ++qb) {
+          const int st = qb % kQS;
+          if (qb >= kQS) mbar_wait_idle(&q_free[st], (qb / kQS - 1) & 1, status);
+          mbar_expect_tx(&q_bar[st], kBoxes * tok * dm.G * 128);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = lane + 32 * e, t = (rb0 + rb) * tok + r / dm.G;
-        v[e] = r < tok * dm.G && t < s.m ? -lse2[(size_t)(s.t0 + t) * dm.Hq + h * dm.G + r % dm.G] : -INFINITY;
+          for (int e = 0; e < kBoxes; ++e) tma_load_3d(Qs + st * kTB + e * kHalfBytes, &tmQ, 64 * e, x.h * dm.G, x.s.t0 + (x.rb0 + rb) * tok, &q_bar[st]);
+        }
+        mbar_arrive(&item_free[c & 1]);
       }
-      if (rb >= kStatStages) mbar_wait_idle(&st_free[ss], (rb / kStatStages - 1) & 1, status);
+    }
+  } else if (warp == 19) {
+    // =============================== the rows' statistics (the warp) ===============================
+    int qb = 0;
+    for (int c = 0;; ++c) {
+      mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status);
+      const Item x = items[c & 1];
+      if (x.b < 0) break;
+      const float* src = lse2 + stat_at(dm, x.s, x.h, x.rb0 * tok * dm.G);
+      const int rows = tok * dm.G;
+      int left = (x.s.m - x.rb0 * tok) * dm.G;  // rows of the pair from this block on
+      // (the next block's statistics are on their way while this one's wait for their place: fetched only then, a block took 3 200
+      // cycles, twice what its exponentials take)
+      float v[4], w[4];
+      auto fetch = [&](float (&to)[4]) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) Ss[ss * kTile + lane + 32 * e] = v[e];
+        for (int e = 0; e < 4; ++e) {
+          const int r = lane + 32 * e;
+          to[e] = r < rows && r < left ? -src[r] : -INFINITY;
+        }
+        src += rows;
+        left -= rows;
+      };
+      fetch(v);
+      for (int rb = 0; rb < x.blocks; ++rb, ++qb) {
+        const int ss = qb % kStatStages;
+        if (rb + 1 < x.blocks) fetch(w);
+        if (qb >= kStatStages) mbar_wait_idle(&st_free[ss], (qb / kStatStages - 1) & 1, status);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) Ss[ss * kTile + lane + 32 * e] = v[e];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&st_bar[ss]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = w[e];
+      }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&st_bar[ss]);
+      if (lane == 0) mbar_arrive(&item_free[c & 1]);
     }
   } else if (warp == 16) {
     // =============================== products (one lane) ===============================
     if (ptx::elect_one()) {
       constexpr uint32_t kIdesc = instr_desc_n(false, kTile);
-      const uint64_t kd0 = smem_desc(smem_u32(Ks), 16, 1024);
-      mbar_wait_idle(k_bar, 0, status);
-      for (int rb = 0; rb < blocks; ++rb) {
-        const int buf = rb & 1, st = rb % kQStages;
-        mbar_wait_idle(&q_bar[st], (rb / kQStages) & 1, status);
-        if (rb >= 2) mbar_wait_idle(&s_free[buf], ((rb - 2) >> 1) & 1, status);
-        tc_fence_after();
-        const uint64_t qd0 = smem_desc(smem_u32(Qs + st * kTB), 16, 1024);
-        for (int kk = 0; kk < tiles; ++kk) {
+      int qb = 0;
+      for (int c = 0;; ++c) {
+        mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status);
+        const int b = items[c & 1].b, blocks = items[c & 1].blocks;
+        if (b < 0) break;
+        const int tiles = items[c & 1].j0 + kTile < items[c & 1].s.n ? 2 : 1;
+        const uint64_t kd0 = smem_desc(smem_u32(Ks + 2 * (c & 1) * kTB), 16, 1024);
+        for (int rb = 0; rb < blocks; ++rb, ++qb) {
+          const int buf = qb & 1, st = qb % kQS;
+          mbar_wait_idle(&q_bar[st], (qb / kQS) & 1, status);
+          if (qb >= 2) mbar_wait_idle(&s_free[buf], ((qb - 2) >> 1) & 1, status);
+          tc_fence_after();
+          const uint64_t qd0 = smem_desc(smem_u32(Qs + st * kTB), 16, 1024);
+          for (int kk = 0; kk < tiles; ++kk) {
 #pragma unroll
-          for (int ks = 0; ks < kSteps; ++ks)
-            umma(tmem + kk * 256 + buf * 128, kd0 + (uint64_t)((kk * kTB) >> 4) + k_major_step(ks), qd0 + k_major_step(ks), kIdesc, ks > 0);
+            for (int ks = 0; ks < kSteps; ++ks)
+              umma(tmem + kk * 256 + buf * 128, kd0 + (uint64_t)((kk * kTB) >> 4) + k_major_step(ks), qd0 + k_major_step(ks), kIdesc, ks > 0);
+          }
+          umma_commit(&q_free[st]);
+          if (rb + 1 == blocks) umma_commit(&item_free[c & 1]);
+          umma_commit(&s_bar[buf]);
         }
-        if (rb + kQStages < blocks) umma_commit(&q_free[st]);
-        umma_commit(&s_bar[buf]);
       }
+      // (no arrival may still be on its way to this CTA's barriers when the CTA ends)
+      if (qb > 0) mbar_wait_idle(&q_free[(qb - 1) % kQS], ((qb - 1) / kQS) & 1, status);
     }
   } else {
     // =============================== two threads per key ===============================
     const float scale2 = dm.scale * kLog2e;
-    const int kk = (warp >> 2) & 1, rh = warp >> 3, key = tid & (kKeys - 1), j = j0 + key;
-    const int need = (j - first) * dm.G;  // the first of the pair's rows that sees the key
+    const int kk = (warp >> 2) & 1, rh = warp >> 3, key = tid & (kKeys - 1);
     const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kk * 256 + rh * 64;
-    float total = 0.f, low = 0.f;  // the sum over row blocks, and what its additions lost
-    for (int rb = 0; rb < blocks; ++rb) {
-      const int buf = rb & 1, ss = rb % kStatStages, r0 = (rb0 + rb) * tok * dm.G + rh * 64;
-      // rows of the block that see the key; masked: not all of them for all keys of this CTA
-      const int lo = need - r0, hi = min(tok, s.m - (rb0 + rb) * tok) * dm.G - rh * 64;
-      const bool masked = (rb0 + rb) * tok < j0 + kKeys - 1 - first || hi < 64;
-      mbar_wait(&s_bar[buf], (rb >> 1) & 1, status);
-      mbar_wait(&st_bar[ss], (rb / kStatStages) & 1, status);
-      tc_fence_after();
-      float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-      uint32_t va[16], vb[16];
-      float4 sa[4], sb[4];
-      const float* stat = Ss + ss * kTile + rh * 64;
-      // two register sets take turns: the next 16 rows' logits and statistics are on their way while these are summed
-      tmem_ld16_issue(t_lane + buf * 128, va);
-      lds16_issue(stat, sa);
-      tmem_ld16_wait(va);
-      tmem_ld16_issue(t_lane + buf * 128 + 16, vb);
-      lds16_issue(stat + 16, sb);
-      add_weights(va, sa, scale2, masked, lo, hi, acc);
-      tmem_ld16_wait(vb);
-      tmem_ld16_issue(t_lane + buf * 128 + 32, va);
-      lds16_issue(stat + 32, sa);
-      add_weights(vb, sb, scale2, masked, lo - 16, hi - 16, acc);
-      tmem_ld16_wait(va);
-      tmem_ld16_issue(t_lane + buf * 128 + 48, vb);
-      lds16_issue(stat + 48, sb);
-      add_weights(va, sa, scale2, masked, lo - 32, hi - 32, acc);
-      tmem_ld16_wait(vb);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s_free[buf]);
-      add_weights(vb, sb, scale2, masked, lo - 48, hi - 48, acc);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&st_free[ss]);
-      const float x = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) - low;
-      const float t = total + x;
-      low = (t - total) - x;
-      total = t;
-    }
-    if (rh == 1) half[key] = total;
-    asm volatile("bar.sync 1, %0;" ::"n"(kKeyThreads) : "memory");
-    if (rh == 0 && j < s.n) {
-      total += half[key];
-      if (kPaged) mass[pool_row(dm, sq, b, h, j, status)] += total;
-      else mass[(size_t)(s.t0 + j) * dm.Hkv + h] = total;
+    int qb = 0;
+    for (int c = 0;; ++c) {
+      mbar_wait(&k_bar[c & 1], (c >> 1) & 1, status);
+      const Item x = items[c & 1];
+      if (x.b < 0) break;
+      const int j = x.j0 + key, first = x.s.n - x.s.m;
+      const int need = (j - first) * dm.G;  // the first of the pair's rows that sees the key
+      // where the sum goes, and what is there already: fetched now, used at the end
+      float* out = nullptr;
+      float total = 0.f, low = 0.f;  // the sum over row blocks, and what its additions lost
+      float before = 0.f;
+      if (rh == 0 && j < x.s.n) {
+        if (kPaged) {
+          out = mass + pool_row(dm, sq, x.b, x.h, j, status);
+          before = *out;
+        } else {
+          out = mass + (size_t)(x.s.t0 + j) * dm.Hkv + x.h;
+        }
+      }
+      for (int rb = 0; rb < x.blocks; ++rb, ++qb) {
+        const int buf = qb & 1, ss = qb % kStatStages, i0 = (x.rb0 + rb) * tok;
+        // rows of the half block that see the key; masked: not all 64 of them for all keys of the item
+        const int lo = need - i0 * dm.G - rh * 64, hi = min(tok, x.s.m - i0) * dm.G - rh * 64;
+        const bool masked = i0 < x.j0 + kKeys - 1 - first || hi < 64;
+        mbar_wait(&s_bar[buf], (qb >> 1) & 1, status);
+        mbar_wait(&st_bar[ss], (qb / kStatStages) & 1, status);
+        tc_fence_after();
+        float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        uint32_t va[16], vb[16];
+        float4 sa[4], sb[4];
+        const float* stat = Ss + ss * kTile + rh * 64;
+        const uint32_t t_s = t_lane + buf * 128;
+        if (!masked) {
+          // two register sets take turns: the next 16 rows' logits and statistics are on their way while these are summed
+          tmem_ld16_issue(t_s, va);
+          lds16_issue(stat, sa);
+          tmem_ld16_wait(va);
+          tmem_ld16_issue(t_s + 16, vb);
+          lds16_issue(stat + 16, sb);
+          add_weights<false>(va, sa, scale2, 0, 0, acc);
+          tmem_ld16_wait(vb);
+          tmem_ld16_issue(t_s + 32, va);
+          lds16_issue(stat + 32, sa);
+          add_weights<false>(vb, sb, scale2, 0, 0, acc);
+          tmem_ld16_wait(va);
+          tmem_ld16_issue(t_s + 48, vb);
+          lds16_issue(stat + 48, sb);
+          add_weights<false>(va, sa, scale2, 0, 0, acc);
+          tmem_ld16_wait(vb);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_free[buf]);
+          add_weights<false>(vb, sb, scale2, 0, 0, acc);
+        } else {
+#pragma unroll 1
+          for (int e = 0; e < 64 && e < hi; e += 16) {  // (a block of few rows is mostly padding)
+            tmem_ld16_issue(t_s + e, va);
+            lds16_issue(stat + e, sa);
+            tmem_ld16_wait(va);
+            add_weights<true>(va, sa, scale2, lo - e, hi - e, acc);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_free[buf]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&st_free[ss]);
+        const float y = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) - low;
+        const float t = total + y;
+        low = (t - total) - y;
+        total = t;
+      }
+      // the two warps that share 32 keys meet (two places in turn: a warp is at most one item ahead of its partner)
+      if (rh == 1) half[(c & 1) * kKeys + key] = total;
+      asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 7)) : "memory");
+      if (out) *out = before + (total + half[(c & 1) * kKeys + key]);
+      if (lane == 0) mbar_arrive(&item_free[c & 1]);
     }
   }
   tc_fence_before();
