@@ -62,14 +62,17 @@ struct Scratch {
   float* lse2;   // [Hkv, T, G] log2-domain log-sum-exp of every row
   float* lpart;  // [splits, T, Hq] and
   float* opart;  // [splits, T, Hq, D]: what the splits of the keys contribute
+  tcore::SplitNote* notes;  // [1 + SMs] which items' keys were split
   few::Records rec;
 };
 constexpr int kMostSplits = 16;
 constexpr int kItemCounter = 12;  // word of the workspace header
-// Splits are only made where the row blocks of a call leave room (two CTAs of 64 rows per SM, or one of 256), so splits x rows
-// stays below what these hold; a bound that grows with T and does not depend on how the rows lie.
-static long long split_rows(const PDims& dm) {
-  const long long rows = (long long)dm.T * dm.Hq, most = 256LL * g_sm_count;
+// fp32: splits are only made where the row blocks of a call leave room for two CTAs of 64 rows per SM, so splits x rows stays
+// below what these hold; a bound that grows with T and does not depend on how the rows lie. bf16: 256 rows of the last round's
+// items per SM.
+static long long split_rows(const PDims& dm, int dtype) {
+  const long long rows = (long long)dm.T * dm.Hq, most = 128LL * g_sm_count;
+  if (dtype == CAOTE_BF16) return 256LL * g_sm_count;
   return rows * kMostSplits < most ? rows * kMostSplits : most;
 }
 // Calls with few rows per sequence over pages take the kernels of paged_decode.cuh: up to kFewRows rows of a pair. Single tokens of
@@ -89,8 +92,9 @@ static size_t carve(const PDims& dm, int dtype, char* base, Scratch* out) {
   };
   Scratch s;
   s.lse2 = take((size_t)dm.T * dm.Hq);
-  s.lpart = take((size_t)split_rows(dm));
-  s.opart = take((size_t)split_rows(dm) * dm.D);
+  s.lpart = take((size_t)split_rows(dm, dtype));
+  s.opart = take((size_t)split_rows(dm, dtype) * dm.D);
+  s.notes = reinterpret_cast<tcore::SplitNote*>(take(4 * (size_t)(1 + g_sm_count)));
   size_t most = off;
   if (dtype == CAOTE_BF16 && dm.max_pages > 0) {
     // (a workspace for more rows per sequence serves calls with fewer: sized for the most rows that come here)
@@ -199,23 +203,22 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
   if (!rc && mass) rc = allow_smem(tcore::mass_kernel<D, kPaged>, tcore::mass_smem<D>());
   if (rc) return rc;
   const int tok = tcore::kTile / dm.G;
-  const long long blocks = (dm.T + dm.B * (2LL * tok - 1)) / (2 * tok), cap = (long long)dm.max_pages << dm.page_shift;
-  long long splits = g_sm_count / (blocks * dm.Hkv);
-  if (splits > cap / tcore::kTile / tcore::kLeastTiles) splits = cap / tcore::kTile / tcore::kLeastTiles;
-  if (splits > kMostSplits) splits = kMostSplits;
-  if (splits < 1) splits = 1;
+  const long long items = (dm.T + dm.B * (2LL * tok - 1)) / (2 * tok) * dm.Hkv, cap = (long long)dm.max_pages << dm.page_shift;
+  // Keys are split where a last round would leave SMs idle and there are keys to split. Prompts of many rounds end with short
+  // items as it is.
+  const long long tiles = ((kPaged ? cap : dm.max_new) + tcore::kTile - 1) / tcore::kTile;
+  const int most_splits = tiles >= 2 * tcore::kLeastTiles && (kPaged || items < 2 * g_sm_count) ? kMostSplits : 1;
   // (items of the mass kernel are numbered in 32 bits)
   const long long key_blocks = (kPaged ? (cap + tcore::kKeys - 1) / tcore::kKeys * dm.B : (long long)dm.T / tcore::kKeys + dm.B) * dm.Hkv;
-  if (blocks > 0x7fffffffLL || key_blocks > 0x7fff0000LL) return CAOTE_ERR_UNSUPPORTED;
+  if (items > 0x7fff0000LL || key_blocks > 0x7fff0000LL) return CAOTE_ERR_UNSUPPORTED;
   CAOTE_LAUNCH("paged_attend_kernel", st,
-               launch_pdl(tcore::attend_kernel<D, kPaged>, dim3((unsigned)blocks, dm.Hkv, (unsigned)splits), dim3(tcore::kAttendThreads),
-                          tcore::attend_smem<D>(), st, tmQ, tmK, tmV, dm, sq, box, (__nv_bfloat16*)o, lse, sc.lse2, sc.opart, sc.lpart, status + kItemCounter,
-                          status));
-  if (splits > 1)
+               launch_pdl(tcore::attend_kernel<D, kPaged>, dim3((unsigned)(items + (most_splits > 1 ? g_sm_count : 0))),
+                          dim3(tcore::kAttendThreads), tcore::attend_smem<D>(), st, tmQ, tmK, tmV, dm, sq, box, (__nv_bfloat16*)o, lse, sc.lse2,
+                          sc.opart, sc.lpart, sc.notes, g_sm_count, most_splits, status + kItemCounter, status));
+  if (most_splits > 1)
     CAOTE_LAUNCH("paged_combine", st,
-                 launch_pdl(generic::combine_kernel<__nv_bfloat16, D>, dim3((unsigned)(((long long)dm.T * dm.Hq + 7) / 8)), dim3(256), 0, st, dm,
-                            sq, (int)splits, tcore::kTile, tcore::kLeastTiles, (const float*)sc.opart, (const float*)sc.lpart,
-                            (__nv_bfloat16*)o, lse, sc.lse2));
+                 launch_pdl(tcore::combine_kernel<D>, dim3(g_sm_count, 8), dim3(256), 0, st, dm, sq, (__nv_bfloat16*)o, lse, sc.lse2,
+                            (const float*)sc.opart, (const float*)sc.lpart, (const tcore::SplitNote*)sc.notes));
   if (mass)
     CAOTE_LAUNCH("paged_mass_kernel", st,
                  launch_pdl(tcore::mass_kernel<D, kPaged>, dim3(g_sm_count), dim3(tcore::kMassThreads), tcore::mass_smem<D>(), st, tmQ, tmK, dm,

@@ -50,31 +50,62 @@ __device__ __forceinline__ Seq sequence(const PDims& dm, const Seqs& sq, int b, 
 // Where the statistic of query row r of a pair lies in the workspace: [Hkv][T][G], so that a block of rows is contiguous.
 __device__ __forceinline__ size_t stat_at(const PDims& dm, const Seq& s, int h, int r) { return ((size_t)h * dm.T + s.t0) * dm.G + r; }
 
-// Work is numbered over all sequences: sequence b has ceil(what(b) / per) blocks. The sequence that block `index` belongs to
-// and its number in there; false: no such block. For one whole warp, the same result in all lanes.
+// Work is numbered over all sequences: a sequence has ceil(what / per) blocks of it, what = its new tokens or its keys. A scan holds
+// one sequence per lane (32 at a time); for one whole warp.
+struct Scan {
+  Seq s;           // this lane's sequence
+  int mine, incl;  // its blocks, and those of all lanes up to it
+  int total;       // blocks of these 32 sequences
+};
 template <typename What>
-__device__ __forceinline__ bool locate(int B, int per, int index, What what, int& b_out, int& block_out) {
+__device__ __forceinline__ Scan scan(const PDims& dm, const Seqs& sq, int b0, int per, What what, int* status) {
   const int lane = threadIdx.x & 31;
-  int base = 0;
-  for (int b0 = 0; b0 < B; b0 += 32) {
-    const int b = b0 + lane;
-    const int mine = b < B ? (what(b) + per - 1) / per : 0;
-    int incl = mine;
+  Scan c;
+  c.s.t0 = c.s.m = c.s.n = 0;
+  if (b0 + lane < dm.B) c.s = sequence(dm, sq, b0 + lane, status);
+  c.mine = (what(c.s) + per - 1) / per;
+  c.incl = c.mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += t;
-    }
-    const unsigned reach = __ballot_sync(0xffffffffu, index < base + incl);
+  for (int o = 1; o < 32; o <<= 1) {
+    const int t = __shfl_up_sync(0xffffffffu, c.incl, o);
+    if (lane >= o) c.incl += t;
+  }
+  c.total = __shfl_sync(0xffffffffu, c.incl, 31);
+  return c;
+}
+// All blocks; `c` holds the first 32 sequences' scan afterwards.
+template <typename What>
+__device__ __forceinline__ int count_blocks(const PDims& dm, const Seqs& sq, int per, What what, int* status, Scan& c) {
+  c = scan(dm, sq, 0, per, what, status);
+  int total = c.total;
+  for (int b0 = 32; b0 < dm.B; b0 += 32) total += scan(dm, sq, b0, per, what, status).total;
+  return total;
+}
+// The sequence that block `index` belongs to, and its number in there, from the first scan on; false: no such block. The same
+// result in all lanes.
+struct Place {
+  int b, block, blocks;  // blocks: of the sequence
+  Seq s;
+};
+template <typename What>
+__device__ __forceinline__ bool find_block(const PDims& dm, const Seqs& sq, int per, int index, What what, Scan c, Place& p) {
+  for (int b0 = 0;;) {
+    const unsigned reach = __ballot_sync(0xffffffffu, index < c.incl);
     if (reach) {
       const int f = __ffs((int)reach) - 1;
-      b_out = b0 + f;
-      block_out = index - (base + __shfl_sync(0xffffffffu, incl - mine, f));
+      p.b = b0 + f;
+      p.blocks = __shfl_sync(0xffffffffu, c.mine, f);
+      p.block = index - (__shfl_sync(0xffffffffu, c.incl, f) - p.blocks);
+      p.s.t0 = __shfl_sync(0xffffffffu, c.s.t0, f);
+      p.s.m = __shfl_sync(0xffffffffu, c.s.m, f);
+      p.s.n = __shfl_sync(0xffffffffu, c.s.n, f);
       return true;
     }
-    base += __shfl_sync(0xffffffffu, incl, 31);
+    index -= c.total;
+    b0 += 32;
+    if (b0 >= dm.B) return false;
+    c = scan(dm, sq, b0, per, what, nullptr);
   }
-  return false;
 }
 
 // Row of the pools' [pages * Hkv * page] rows that holds slot j of sequence b for KV head h. A page outside the pool is

@@ -111,18 +111,14 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
   // all tiles, and (one warp of the launch) where the sequences begin
   const bool writes_plan = blockIdx.x == 0 && warp == 0;
   const int workers = gridDim.x * kWarps, w = warp * gridDim.x + blockIdx.x;
-  int W = 0;
-  for (int b0 = 0; b0 < dm.B; b0 += 32) {
-    const int b = b0 + lane;
-    const int mine = b < dm.B ? tiles_of(sequence(dm, sq, b, writes_plan ? status : nullptr)) * dm.Hkv : 0;
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += t;
-    }
-    if (writes_plan && b < dm.B) rec.plan[b] = W + incl - mine;
-    W += __shfl_sync(0xffffffffu, incl, 31);
+  auto what = [&](const Seq& s) { return tiles_of(s) * dm.Hkv; };
+  Scan first = scan(dm, sq, 0, 1, what, writes_plan ? status : nullptr);
+  if (writes_plan && lane < dm.B) rec.plan[lane] = first.incl - first.mine;
+  int W = first.total;
+  for (int b0 = 32; b0 < dm.B; b0 += 32) {
+    const Scan c = scan(dm, sq, b0, 1, what, writes_plan ? status : nullptr);
+    if (writes_plan && b0 + lane < dm.B) rec.plan[b0 + lane] = W + c.incl - c.mine;
+    W += c.total;
   }
   const int per = max((W + workers - 1) / workers, kLeast);
   if (writes_plan && lane == 0) {
@@ -135,12 +131,13 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 
   Cursor c;
   {
-    int x = 0;
-    locate(dm.B, 1, (int)begin, [&](int b) { return tiles_of(sequence(dm, sq, b)) * dm.Hkv; }, c.b, x);
-    c.s = sequence(dm, sq, c.b);
+    Place p;
+    find_block(dm, sq, 1, (int)begin, what, first, p);
+    c.b = p.b;
+    c.s = p.s;
     c.tiles = tiles_of(c.s);
-    c.h = x / c.tiles;
-    c.tile = x % c.tiles;
+    c.h = p.block / c.tiles;
+    c.tile = p.block % c.tiles;
   }
   // ---- copies, a few tiles ahead: lane l of `ids` holds the page of tile ids_from + l of the cursor's pair ----
   Cursor p = c;

@@ -95,9 +95,11 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
   int* where = reinterpret_cast<int*>(Ps + kRows<RPT> * kP);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = blockIdx.y, split = blockIdx.z;
   if (tid < 32) {
-    int b = -1, block = 0;
-    if (!locate(dm.B, kRows<RPT>, blockIdx.x, [&](int x) { return sequence(dm, sq, x).m * dm.G; }, b, block)) b = -1;
-    if (tid == 0) { where[0] = b; where[1] = block; }
+    auto what = [&](const Seq& x) { return x.m * dm.G; };
+    Place p;
+    Scan c = scan(dm, sq, 0, kRows<RPT>, what, nullptr);
+    const bool there = find_block(dm, sq, kRows<RPT>, blockIdx.x, what, c, p);
+    if (tid == 0) { where[0] = there ? p.b : -1; where[1] = p.block; }
     if (blockIdx.x == 0 && h == 0 && split == 0)
       for (int x = tid; x < dm.B; x += 32) sequence(dm, sq, x, status);
   }
@@ -269,9 +271,11 @@ mass_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ K,
   int* where = reinterpret_cast<int*>(Ps + kRows<RPT> * kP);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = blockIdx.y;
   if (tid < 32) {
-    int b = -1, block = 0;
-    if (!locate(dm.B, kKeys, blockIdx.x, [&](int x) { const Seq s = sequence(dm, sq, x); return s.m > 0 ? s.n : 0; }, b, block)) b = -1;
-    if (tid == 0) { where[0] = b; where[1] = block; }
+    auto what = [&](const Seq& x) { return x.m > 0 ? x.n : 0; };
+    Place p;
+    Scan c = scan(dm, sq, 0, kKeys, what, nullptr);
+    const bool there = find_block(dm, sq, kKeys, blockIdx.x, what, c, p);
+    if (tid == 0) { where[0] = there ? p.b : -1; where[1] = p.block; }
   }
   __syncthreads();
   const int b = where[0], j0 = where[1] * kKeys;

@@ -2,9 +2,10 @@
 //
 //   attend_kernel   rows x keys. A CTA owns two blocks of up to 128 query rows of a (sequence, KV head) pair (a block: 128 / G
 //                   tokens with all G heads) and walks the keys that they see in tiles of 128, K and V of a tile read once for
-//                   both blocks. S = Q K^T into TMEM; a thread per row takes its 128 logits out of TMEM, keeps running maximum
-//                   and sum, and writes its numerators P as bf16 over the S it came from; O += P V with P as the TMEM-side A
-//                   operand. The two blocks take turns: while one's logits are being exponentiated, the other's products run.
+//                   both blocks. S = Q K^T into TMEM; a thread per row takes its logits out of TMEM, keeps a reference and the
+//                   sum, and writes its numerators P as bf16 over the S it came from, 64 keys at a time; O += P V with P as
+//                   the TMEM-side A operand. The two blocks take turns: while one's logits are being exponentiated, the
+//                   other's products run.
 //   mass_kernel     keys x rows. A CTA owns 256 keys of a pair and walks the rows that see them: S^T = K Q^T into TMEM, one key
 //                   per lane, so that a thread sums 2^(s - lse) over the rows of its own key without any exchange.
 //
@@ -31,13 +32,15 @@ using namespace caote::tc;
 using ptx::tma_load_3d;
 
 constexpr int kLeastTiles = 4;  // key tiles per split
+constexpr int kPolyOf = 4;      // of so many pairs of exponentials one goes to the FMA pipe (none: 239, one of four: 230 us, 12 001 prompt tokens)
 template <int D>
 constexpr int kKStages = D == 128 ? 2 : 4;
 template <int D>
 constexpr int kVStages = D == 128 ? 3 : 4;
-constexpr int kAttendThreads = 256 + 96;  // a thread per row of two blocks; warps for products, K copies, V copies
+constexpr int kRowThreads = 512;                  // two threads per row of two blocks
+constexpr int kAttendThreads = kRowThreads + 96;  // and warps for products, Q and K copies, V copies
 template <int D>
-constexpr size_t attend_smem() { return 1024 + (size_t)(2 + kKStages<D> + kVStages<D>) * kTileBytesOf<D> + 512; }
+constexpr size_t attend_smem() { return 1024 + (size_t)(2 + kKStages<D> + kVStages<D>) * kTileBytesOf<D> + 2 * kTile * sizeof(float) + 512; }
 
 // Tiles of 128 keys come as boxes of `box` tokens: min(page, 128), prompts 128. Lane l of a warp copies box l of a tile.
 // The page of this lane's box of the tile at slot j0 (of no meaning behind the length).
@@ -73,13 +76,36 @@ __device__ __forceinline__ void copy_keys(const PDims& dm, const CUtensorMap* tm
   __syncwarp();
 }
 
-// grid = (pairs of row blocks of all sequences, Hkv, splits). lse2: the rows' statistics for the mass (stat_at); with more than one
-// split opart, lpart as in generic::attend_kernel.
+// Work is numbered in items: a pair of row blocks of one KV head, the heads in turn, a sequence's longest first. Whole rounds of
+// items, one per SM, are taken as they are; the keys of the last items, fewer than SMs, are split among the SMs (most_splits > 1).
+struct Schedule {
+  int items, whole, splits;  // items [whole, items) are cut into `splits`
+};
+__device__ __forceinline__ Schedule schedule(const PDims& dm, int per_head, int sms, int most_splits) {
+  Schedule c;
+  c.items = per_head * dm.Hkv;
+  c.whole = c.items / sms * sms;
+  c.splits = c.items > c.whole ? min(most_splits, sms / (c.items - c.whole)) : 1;
+  return c;
+}
+// What a CTA works on.
+struct Where {
+  int b, i0, h;           // sequence (-1: nothing), first token, KV head
+  int split, splits, x;   // split of the keys of how many, place behind the whole items
+  Seq s;
+};
+// What combine_kernel needs to know, left by attend_kernel: [0] = (split items, splits), [1 + i] = (sequence, first token, KV head,
+// splits in use) of split item i.
+typedef int4 SplitNote;
+
+// grid: CTA x takes item x, or behind the whole ones split (x - whole) % splits of item whole + (x - whole) / splits. lse2: the
+// rows' statistics for the mass (stat_at); a split leaves its rows' normalised outputs and statistics at opart, lpart
+// [x - whole][256 rows].
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kAttendThreads, 1)
 attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               PDims dm, Seqs sq, int box, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ lse2,
-              float* __restrict__ opart, float* __restrict__ lpart, int* next_item, int* status) {
+              float* __restrict__ opart, float* __restrict__ lpart, SplitNote* __restrict__ notes, int sms, int most_splits, int* next_item, int* status) {
   constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16, kKS = kKStages<D>, kVS = kVStages<D>;
   ptx::pdl_wait();
   ptx::pdl_trigger();
@@ -89,54 +115,62 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   char* Qs = sm;                  // [2]
   char* Ks = Qs + 2 * kTB;        // [kKS]
   char* Vs = Ks + kKS * kTB;      // [kVS]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(Vs + kVS * kTB);
+  float* xch = reinterpret_cast<float*>(Vs + kVS * kTB);  // [2][kTile] a row's maximum on its way between its two threads
+  uint64_t* bars = reinterpret_cast<uint64_t*>(xch + 2 * kTile);
   uint64_t *q_bar = &bars[0], *k_bar = &bars[1], *v_bar = k_bar + kKS, *k_free = v_bar + kVS, *v_free = k_free + kKS,
-           *s_bar = v_free + kVS, *o_bar = s_bar + 2, *p_bar = o_bar + 2;  // p_bar: [block][part]
-  constexpr int kBars1 = 1 + 2 * (kKS + kVS) + 4;
+           *s_bar = v_free + kVS, *h_bar = s_bar + 2, *o_bar = h_bar + 2, *p_bar = o_bar + 2;  // p_bar: [block][part]
+  constexpr int kBars1 = 1 + 2 * (kKS + kVS) + 6;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars1 + 4);
-  int* where = reinterpret_cast<int*>(tmem_slot + 1);
+  Where* where = reinterpret_cast<Where*>(tmem_slot + 1);
 
-  const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index(), h = blockIdx.y, split = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
   const int tok = kTile / dm.G;  // tokens per row block
+  // three warps set up side by side: which item, barriers, TMEM
   if (warp == 0) {
-    int b = -1, block = 0;
-    if (!locate(dm.B, 2 * tok, blockIdx.x, [&](int x) { return sequence(dm, sq, x).m; }, b, block)) b = -1;
-    if (lane == 0) { where[0] = b; where[1] = block; }
-  } else if (warp == 1 && blockIdx.x == 0 && h == 0 && split == 0) {
-    for (int x = lane; x < dm.B; x += 32) sequence(dm, sq, x, status);
-    if (lane == 0) *next_item = 0;  // (for the mass kernel)
-  }
-  if (tid == 0) {
+    auto what = [](const Seq& x) { return x.m; };
+    Scan first;
+    const Schedule c = schedule(dm, count_blocks(dm, sq, 2 * tok, what, blockIdx.x == 0 ? status : nullptr, first), sms, most_splits);
+    const int x = blockIdx.x - c.whole, item = x < 0 ? blockIdx.x : c.whole + x / c.splits;
+    Place p;
+    const bool there = item < c.items && find_block(dm, sq, 2 * tok, item / dm.Hkv, what, first, p);
+    if (lane == 0) {
+      *where = Where{there ? p.b : -1, (p.blocks - 1 - p.block) * 2 * tok, item % dm.Hkv, x < 0 ? 0 : x % c.splits, x < 0 ? 1 : c.splits, x, p.s};
+      if (blockIdx.x == 0) {
+        *next_item = 0;  // (for the mass kernel)
+        notes[0] = make_int4(c.splits > 1 ? c.items - c.whole : 0, c.splits, 0, 0);
+      }
+    }
+  } else if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+  } else if (tid == 64) {
     for (int i = 0; i < kBars1; ++i) mbar_init(&bars[i], 1);
-    for (int i = 0; i < 4; ++i) mbar_init(&p_bar[i], 4);
+    for (int i = 0; i < 4; ++i) mbar_init(&p_bar[i], 8);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  tc_fence_before();
   __syncthreads();
-  const int b = where[0];
-  if (b < 0) return;
-  const Seq s = sequence(dm, sq, b);
+  tc_fence_after();
+  // columns: S (and P) of block i at 128 i, O at 256 + 128 i
+  const uint32_t tmem = *tmem_slot;
+  const int b = where->b, i0 = where->i0, h = where->h, split = where->split;
+  const Seq s = where->s;
   const int first = s.n - s.m;  // token i sees slots up to first + i
-  // blocks with most keys first: the last CTAs of a launch are short ones
-  const int i0 = ((s.m + 2 * tok - 1) / (2 * tok) - 1 - where[1]) * 2 * tok;
-  int per, count;
-  key_splits((s.n + kTile - 1) / kTile, gridDim.z, kLeastTiles, per, count);
-  if (split >= count) return;
+  int per = 1, count = 0;
+  if (b >= 0) key_splits((s.n + kTile - 1) / kTile, where->splits, kLeastTiles, per, count);
+  if (split == 0 && where->splits > 1 && b >= 0 && tid == 0) notes[1 + where->x / where->splits] = make_int4(b, i0, h, count);
+  if (split >= count) {
+    if (warp == 1) tmem_dealloc(tmem, 512);
+    return;
+  }
   // this CTA's tiles [kt0, kt0 + c) for either block
   const int kt0 = split * per;
   const int c0 = min(per, (first + min(i0 + tok, s.m) - 1) / kTile + 1 - kt0);
   const int c1 = i0 + tok < s.m ? min(per, (first + min(i0 + 2 * tok, s.m) - 1) / kTile + 1 - kt0) : 0;
   const int tiles = max(max(c0, c1), 0);
 
-  if (warp == 0) tmem_alloc(tmem_slot, 512);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  // columns: S (and P) of block i at 128 i, O at 256 + 128 i
-  const uint32_t tmem = *tmem_slot;
-
-  if (warp >= 9) {
-    // =============================== copies: warp 9 Q and K, warp 10 V ===============================
-    const bool is_v = warp == 10;
+  if (warp >= 17) {
+    // =============================== copies: warp 17 Q and K, warp 18 V ===============================
+    const bool is_v = warp == 18;
     const CUtensorMap* tm = is_v ? &tmV : &tmK;
     char* ring = is_v ? Vs : Ks;
     uint64_t *full = is_v ? v_bar : k_bar, *free = is_v ? v_free : k_free;
@@ -149,8 +183,8 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         for (int x = 0; x < kBoxes; ++x)
           tma_load_3d(Qs + i * kTB + x * kHalfBytes, &tmQ, 64 * x, h * dm.G, s.t0 + i0 + i * tok, q_bar);
     }
-    int id = page_of<kPaged>(dm, sq, b, s.n, kt0 * kTile, box, status);
     int st = 0, round = 0;
+    int id = page_of<kPaged>(dm, sq, b, s.n, kt0 * kTile, box, status);
     for (int kt = 0; kt < tiles; ++kt) {
       const int j0 = (kt0 + kt) * kTile;
       const int next = page_of<kPaged>(dm, sq, b, s.n, j0 + kTile, box, status);
@@ -161,7 +195,7 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       id = next;
       if (++st == stages) { st = 0; ++round; }
     }
-  } else if (warp == 8) {
+  } else if (warp == 16) {
     // =============================== products (one lane) ===============================
     if (ptx::elect_one() && tiles > 0) {
       constexpr uint32_t kIdescS = instr_desc_n(false, kTile), kIdescO = instr_desc_n(true, D);
@@ -174,9 +208,9 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const uint64_t qd = qdesc0 + (uint64_t)((i * kTB) >> 4), kd = kdesc0 + (uint64_t)((st * kTB) >> 4);
 #pragma unroll
         for (int ks = 0; ks < kSteps; ++ks) umma(tmem + i * 128, qd + k_major_step(ks), kd + k_major_step(ks), kIdescS, ks > 0);
-        umma_commit(&s_bar[i]);
         // (the last block that reads this K hands its stage back, if anyone waits for it)
         if (kt + kKS < tiles && (i == 1 || kt >= c1)) umma_commit(&k_free[st]);
+        umma_commit(&s_bar[i]);
       };
       mbar_wait(q_bar, 0, status);
       if (c0 > 0) issue_s(0, 0);
@@ -190,12 +224,15 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           mbar_wait(&v_bar[st], (kt / kVS) & 1, status);
           const uint64_t vd = vdesc0 + (uint64_t)((st * kTB) >> 4);
 #pragma unroll
-          for (int part = 0; part < 2; ++part) {  // 64 keys each, as the rows hand them over
+          for (int part = 0; part < 2; ++part) {  // 32 keys of either half, as the rows hand them over
             mbar_wait(&p_bar[2 * i + part], kt & 1, status);
             tc_fence_after();
 #pragma unroll
-            for (int ks = 4 * part; ks < 4 * part + 4; ++ks)
-              umma_ts(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, vd + mn_major_step(ks), kIdescO, kt > 0 || ks > 0);
+            for (int x = 0; x < 4; ++x) {
+              const int ks = (x >> 1) * 4 + 2 * part + (x & 1);
+              umma_ts(tmem + 256 + i * 128, tmem + i * 128 + (ks >> 2) * 64 + (ks & 3) * 8, vd + mn_major_step(ks), kIdescO, kt > 0 || ks > 0);
+            }
+            if (part == 0) umma_commit(&h_bar[i]);
           }
           if (kt + kVS < tiles && (i == 1 || kt >= c1)) umma_commit(&v_free[st]);
           umma_commit(&o_bar[i]);
@@ -205,58 +242,63 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       }
     }
   } else {
-    // =============================== a thread per query row ===============================
-    const int i = warp >> 2, row = tid & 127, c = i ? c1 : c0;
+    // =============================== two threads per query row ===============================
+    // Threads t and t + 128 of a block's 256 share row t: each has 64 of a tile's keys and half of the channels when O is touched.
+    // (A thread per row: a warp alone on its scheduler takes 4 cycles per instruction and twice what the exponentials take.)
+    const int i = warp >> 3, hf = (warp >> 2) & 1, row = tid & 127, c = i ? c1 : c0;
+    const int pair_bar = 1 + i * 4 + (warp & 3);  // the two warps that share 32 rows
     const int tkn = i0 + i * tok + row / dm.G;
     const bool valid = row < tok * dm.G && tkn < s.m;
     const int vis = valid ? first + tkn + 1 : s.n;       // keys this row sees
     const int plain = first + i0 + i * tok + 1;          // ... and every row of the block
     const float scale2 = dm.scale * kLog2e;
-    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + i * 128, t_o = t_s + 256;
+    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + i * 128;
+    const uint32_t t_s = t_lane + hf * 64, t_o = t_lane + 256 + hf * (D / 2);
+    // the larger of a value of this thread and one of the row's other thread
+    auto row_max = [&](float x) {
+      float* at = xch + i * kTile + row;
+      if (hf == 1) *at = x;
+      asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+      if (hf == 0) *at = x = fmaxf(x, *at);
+      asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+      if (hf == 1) x = *at;
+      return x;
+    };
+    // whether any thread of the two warps says so
+    auto any_of_pair = [&](bool x) {
+      uint32_t r;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\t"
+          "setp.ne.u32 q, %1, 0;\n\t"
+          "bar.red.or.pred p, %2, 64, q;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(r) : "r"((uint32_t)x), "r"(pair_bar) : "memory");
+      return r != 0;
+    };
+    // Numerators are 2^(logit - m_ref) for a reference that is left alone until a logit passes it by 2^60: nothing is lost meanwhile
+    // (P, l and O are floats, their ratios do not depend on it), and no maximum stands between a logit and its exponential. The
+    // 32 keys of a part are exponentiated and their maximum is formed at the same time; only where it has passed the mark is the
+    // part done again, with a new reference.
+    constexpr float kMark = 60.f;
     float m_ref = -INFINITY, l = 0.f;
+    const float2 scale22 = make_float2(scale2, scale2);
     for (int kt = 0; kt < c; ++kt) {
       const int j0 = (kt0 + kt) * kTile;
+      const bool masked = j0 + kTile > plain;
+      const int lim = vis - j0 - hf * 64;
       mbar_wait(&s_bar[i], kt & 1, status);
       tc_fence_after();
-      float sv[2][64];
-      tmem_ld64(t_s, sv[0]);
-      tmem_ld64(t_s + 64, sv[1]);
-      if (j0 + kTile > plain) {
-        const int lim = vis - j0;
-#pragma unroll
-        for (int e = 0; e < 128; ++e) sv[e >> 6][e & 63] = e < lim ? sv[e >> 6][e & 63] : -INFINITY;
-      }
-      float mx;
-      {
-        float pm[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) pm[e] = fmaxf(sv[0][e], sv[0][e + 8]);
-#pragma unroll
-        for (int e = 16; e < 128; e += 16) {
-#pragma unroll
-          for (int f = 0; f < 8; ++f) pm[f] = fmaxf(fmaxf(pm[f], sv[e >> 6][(e & 63) + f]), sv[e >> 6][(e & 63) + 8 + f]);
-        }
-        mx = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), fmaxf(fmaxf(pm[4], pm[5]), fmaxf(pm[6], pm[7]))) * scale2;
-      }
-      // the reference moves only when a logit exceeds it by more than 8 (numerators up to 256 in between)
-      const bool need = mx > m_ref + 8.f;
-      float corr = 1.f;
-      if (need) {
-        corr = ptx::fast_exp2(m_ref - mx);
-        m_ref = mx;
-        l *= corr;
-      }
-      if (kt > 0 && __any_sync(0xffffffffu, need)) {
-        // (S of this tile was formed behind O += P V of the tile before)
+      if (kt == 0) {  // the first reference: the largest of the first 32 logits of either half
+        float mx = -INFINITY;
 #pragma unroll 1
-        for (int cc = 0; cc < D / 16; ++cc) {
+        for (int e0 = 0; e0 < 32; e0 += 16) {
           uint32_t v[16];
-          tmem_ld16_issue(t_o + cc * 16, v);
+          tmem_ld16_issue(t_s + e0, v);
           tmem_ld16_wait(v);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * corr);
-          tmem_st16u(t_o + cc * 16, v);
+          for (int e = 0; e < 16; ++e) mx = fmaxf(mx, e0 + e < lim ? __uint_as_float(v[e]) : -INFINITY);
         }
+        m_ref = row_max(mx * scale2);
       }
       const int n_valid = s.n - j0;
       if (n_valid < kTile) {
@@ -266,75 +308,217 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         if (row >= n_valid) {
           char* vt = Vs + (kt % kVS) * kTB;
 #pragma unroll
-          for (int x = 0; x < D / 8; ++x)
+          for (int x = hf * (D / 16); x < (hf + 1) * (D / 16); ++x)
             *reinterpret_cast<uint4*>(vt + (x >> 3) * kHalfBytes + row * 128 + (((x & 7) ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
         }
         ptx::fence_async_smem();
       }
-      const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
-      const float2 scale22 = make_float2(scale2, scale2), neg2 = make_float2(neg, neg);
-      float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
-        uint32_t pk[32];
+        uint32_t pk[16];
+        float2 sum;
+        for (;;) {
+          uint32_t v[32];
+          tmem_ld32_issue(t_s + 32 * part, v);
+          tmem_ld32_wait(v);
+          const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
+          const float2 neg2 = make_float2(neg, neg);
+          if (masked) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float2 x = __ffma2_rn(make_float2(sv[part][2 * e], sv[part][2 * e + 1]), scale22, neg2);
-          const float2 p = make_float2(ptx::fast_exp2(x.x), ptx::fast_exp2(x.y));
-          ls[e & 1] = __fadd2_rn(ls[e & 1], p);
-          pk[e] = pack_bf16(p.x, p.y);
+            for (int e = 0; e < 32; ++e) v[e] = 32 * part + e < lim ? v[e] : 0xff800000u;
+          }
+          float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale22, neg2);
+            const float2 p = e % kPolyOf == kPolyOf - 1 ? poly_exp2x2(x) : make_float2(ptx::fast_exp2(x.x), ptx::fast_exp2(x.y));
+            ls[e & 1] = __fadd2_rn(ls[e & 1], p);
+            pk[e] = pack_bf16(p.x, p.y);
+          }
+          float pm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 8)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) pm[f] = fmaxf(fmaxf(pm[f], __uint_as_float(v[e + f])), __uint_as_float(v[e + f + 4]));
+          const float mx = fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])) * scale2;
+          sum = __fadd2_rn(ls[0], ls[1]);
+          if (!any_of_pair(mx > m_ref + kMark)) break;
+          const float both = row_max(mx);
+          float corr = 1.f;
+          if (both > m_ref + kMark) {
+            corr = ptx::fast_exp2(m_ref - both);
+            m_ref = both;
+            l *= corr;
+          }
+          // O holds all tiles before this one (S of this tile was formed behind their products), and behind the first part
+          // that too
+          if (part == 1) {
+            mbar_wait(&h_bar[i], kt & 1, status);
+            tc_fence_after();
+          }
+          if (kt > 0 || part == 1) {
+#pragma unroll 1
+            for (int cc = 0; cc < D / 32; ++cc) {
+              uint32_t w[16];
+              tmem_ld16_issue(t_o + cc * 16, w);
+              tmem_ld16_wait(w);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * corr);
+              tmem_st16u(t_o + cc * 16, w);
+            }
+          }
         }
-        tmem_st32u(t_s + 32 * part, pk);
+        l += sum.x + sum.y;
+        tmem_st16u(t_s + 16 * part, pk);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_bar[2 * i + part]);
       }
-      l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
     }
     if (c > 0) {
       mbar_wait(&o_bar[i], (c - 1) & 1, status);
       tc_fence_after();
     }
-    // ---- the row's output and statistic ----
+    // ---- the row's output and statistic; rows go out by way of the block's Q tile, which its products are done with, 16 bytes
+    // number c of a row at place c ^ (row & 7) (a thread's own row straight to memory: 32 lines per store) ----
+    {
+      // the sums of the row's two threads
+      float* at = xch + i * kTile + row;
+      if (hf == 1) *at = l;
+      asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+      if (hf == 0) *at = l += *at;
+      asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+      if (hf == 1) l = *at;
+    }
     const float inv = l > 0.f ? 1.f / l : 0.f, stat = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
-    const size_t at = (size_t)(s.t0 + tkn) * dm.Hq + h * dm.G + row % dm.G;
+    char* mine = Qs + i * kTB + (warp & 3) * (kTB / 4);  // the pair's 32 rows
+    auto place = [&](int r, int piece) { return mine + r * (kTB / 128) + ((piece ^ (r & 7)) << 4); };
     if (count == 1) {
-      if (valid) {
+      if (valid && hf == 0) {
         lse2[stat_at(dm, s, h, (i0 + i * tok) * dm.G + row)] = stat;
-        if (lse) lse[at] = stat * kLn2;
+        if (lse) lse[(size_t)(s.t0 + tkn) * dm.Hq + h * dm.G + row % dm.G] = stat * kLn2;
       }
+      if (c > 0) {
 #pragma unroll
-      for (int cc = 0; cc < D / 32; ++cc) {
-        float v[32];
-        tmem_ld32(t_o + cc * 32, v);
-        if (valid) {
-          uint4* dst = reinterpret_cast<uint4*>(o + at * D + cc * 32);
+        for (int cc = 0; cc < D / 64; ++cc) {
+          float v[32];
+          tmem_ld32(t_o + cc * 32, v);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            dst[e] = make_uint4(pack_bf16(v[8 * e] * inv, v[8 * e + 1] * inv), pack_bf16(v[8 * e + 2] * inv, v[8 * e + 3] * inv),
-                                pack_bf16(v[8 * e + 4] * inv, v[8 * e + 5] * inv), pack_bf16(v[8 * e + 6] * inv, v[8 * e + 7] * inv));
+            *reinterpret_cast<uint4*>(place(lane, hf * (D / 16) + cc * 4 + e)) =
+                make_uint4(pack_bf16(v[8 * e] * inv, v[8 * e + 1] * inv), pack_bf16(v[8 * e + 2] * inv, v[8 * e + 3] * inv),
+                           pack_bf16(v[8 * e + 4] * inv, v[8 * e + 5] * inv), pack_bf16(v[8 * e + 6] * inv, v[8 * e + 7] * inv));
+        }
+        asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+        constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;
+#pragma unroll 4
+        for (int r0 = hf * 16; r0 < hf * 16 + 16; r0 += kAtOnce) {
+          const int r = r0 + lane / kPieces, br = (warp & 3) * 32 + r, t = i0 + i * tok + br / dm.G;
+          if (br < tok * dm.G && t < s.m)
+            *reinterpret_cast<uint4*>(o + ((size_t)(s.t0 + t) * dm.Hq + h * dm.G + br % dm.G) * D + lane % kPieces * 8) =
+                *reinterpret_cast<const uint4*>(place(r, lane % kPieces));
         }
       }
     } else {
-      const size_t slot = (size_t)split * dm.T * dm.Hq + at;
-      if (valid) lpart[slot] = stat;
+      // [x][block][half of the channels][row], as they lie in shared memory: the threads of either half in turn
+      const size_t slot = (size_t)where->x * (2 * kTile) + i * kTile;
+      if (valid && hf == 0) lpart[slot + row] = stat;
+      if (c > 0) {
+#pragma unroll 1
+        for (int turn = 0; turn < 2; ++turn) {
+          if (turn == hf) {
 #pragma unroll
-      for (int cc = 0; cc < D / 32; ++cc) {
-        float v[32];
-        if (c > 0) tmem_ld32(t_o + cc * 32, v);
-        if (valid && c > 0) {
+            for (int cc = 0; cc < D / 64; ++cc) {
+              float v[32];
+              tmem_ld32(t_o + cc * 32, v);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<float4*>(opart + slot * D + cc * 32 + e) = make_float4(v[e] * inv, v[e + 1] * inv, v[e + 2] * inv, v[e + 3] * inv);
+              for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<float4*>(place(lane, cc * 8 + e)) = make_float4(v[4 * e] * inv, v[4 * e + 1] * inv, v[4 * e + 2] * inv, v[4 * e + 3] * inv);
+            }
+            ptx::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              ptx::bulk_store(opart + (slot * 2 + hf * kTile + (warp & 3) * 32) * (D / 2), mine, kTB / 4);
+              ptx::bulk_commit();
+              ptx::bulk_wait_read();
+            }
+            __syncwarp();
+          }
+          asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
         }
+        ptx::bulk_wait();
       }
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 0) tmem_dealloc(tmem, 512);
+  if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// o = sum_s o_s 2^(lse_s - lse) over the splits of the rows of split items. grid = (SMs, 8): a CTA has 32 rows of an item, four per
+// warp.
+template <int D>
+__global__ void __launch_bounds__(256)
+combine_kernel(PDims dm, Seqs sq, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ lse2,
+               const float* __restrict__ opart, const float* __restrict__ lpart, const SplitNote* __restrict__ notes) {
+  ptx::pdl_wait();
+  ptx::pdl_trigger();
+  constexpr int CPL = D / 32, kR = 4;
+  const int tok = kTile / dm.G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const SplitNote all = notes[0], it = notes[1 + blockIdx.x];
+  if ((int)blockIdx.x >= all.x || it.w == 1) return;
+  const int t0 = sq.cu[it.x], m = sq.cu[it.x + 1] - t0, i0 = it.y, h = it.z, count = it.w;
+  const int local0 = blockIdx.y * 32 + warp * kR, i = local0 / kTile, row0 = local0 % kTile;
+  const size_t slot = (size_t)blockIdx.x * all.y * (2 * kTile) + local0;
+  // channel k * 32 + lane of row `row0 + e` as attend_kernel left it
+  auto part_at = [&](int sp, int e, int k) {
+    const int ch = k * 32 + lane, row = row0 + e, in_half = ch % (D / 2);
+    const size_t base = ((size_t)blockIdx.x * all.y + sp) * (2 * kTile) + i * kTile;
+    return ((base * 2 + (ch / (D / 2)) * kTile + row) * (D / 2)) + ((((in_half >> 2) ^ (row & 7)) << 2) | (in_half & 3));
+  };
+  float mine[kR];
+#pragma unroll
+  for (int e = 0; e < kR; ++e) {
+    const bool there = row0 + e < tok * dm.G && i0 + i * tok + (row0 + e) / dm.G < m;
+    mine[e] = there && lane < count ? lpart[slot + (size_t)lane * (2 * kTile) + e] : -INFINITY;
+  }
+  float stat[kR], v[kR][CPL];
+#pragma unroll
+  for (int e = 0; e < kR; ++e) {
+    const float top = warp_max(mine[e]);
+    mine[e] = top == -INFINITY ? 0.f : ptx::fast_exp2(mine[e] - top);
+    const float sum = warp_sum(mine[e]);
+    stat[e] = top + __log2f(sum);
+    mine[e] *= 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < CPL; ++k) v[e][k] = 0.f;
+  }
+#pragma unroll 2
+  for (int sp = 0; sp < count; ++sp) {
+#pragma unroll
+    for (int e = 0; e < kR; ++e) {
+      const float w = __shfl_sync(0xffffffffu, mine[e], sp);
+#pragma unroll
+      for (int k = 0; k < CPL; ++k)  // (a split in which the row sees no key has written no output)
+        v[e][k] = fmaf(w, w > 0.f ? opart[part_at(sp, e, k)] : 0.f, v[e][k]);
+    }
+  }
+  Seq s;
+  s.t0 = t0;
+#pragma unroll
+  for (int e = 0; e < kR; ++e) {
+    const int tkn = i0 + i * tok + (row0 + e) / dm.G;
+    if (row0 + e >= tok * dm.G || tkn >= m) continue;
+    const size_t at = (size_t)(t0 + tkn) * dm.Hq + h * dm.G + (row0 + e) % dm.G;
+#pragma unroll
+    for (int k = 0; k < CPL; ++k) o[at * D + k * 32 + lane] = __float2bfloat16_rn(v[e][k]);
+    if (lane == 0) {
+      lse2[stat_at(dm, s, h, (i0 + i * tok) * dm.G + row0 + e)] = stat[e];
+      if (lse) lse[at] = stat[e] * kLn2;
+    }
+  }
 }
 
 // ---- the weight that every key received ------------------------------------------------------------------
@@ -414,7 +598,8 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
 
   if (warp == 17) {
     // =============================== items and their K (the warp) ===============================
-    auto blocks_of_seq = [&](int x) { const Seq s = sequence(dm, sq, x); return s.m > 0 ? s.n : 0; };
+    auto what = [](const Seq& x) { return x.m > 0 ? x.n : 0; };
+    const Scan seqs = scan(dm, sq, 0, kKeys, what, nullptr);
     for (int c = 0;; ++c) {
       const int buf = c & 1;
       int it = 0;
@@ -423,11 +608,12 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       Item x;
       // A prompt's first keys are seen by most rows: the heads take turns, so that what comes last is short. (Head by head the
       // last head's first keys come late: 2.84 instead of 1.4 ms, 64/8 heads, prompts of 7 428 and 8 956 tokens.)
-      int block = 0;
-      if (locate(dm.B, kKeys, it / dm.Hkv, blocks_of_seq, x.b, block)) {
+      Place p;
+      if (find_block(dm, sq, kKeys, it / dm.Hkv, what, seqs, p)) {
+        x.b = p.b;
         x.h = it % dm.Hkv;
-        x.s = sequence(dm, sq, x.b);
-        x.j0 = block * kKeys;
+        x.s = p.s;
+        x.j0 = p.block * kKeys;
         x.rb0 = max(0, x.j0 - (x.s.n - x.s.m)) / tok;
         x.blocks = (x.s.m + tok - 1) / tok - x.rb0;
       } else {
