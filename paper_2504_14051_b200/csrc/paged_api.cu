@@ -75,12 +75,14 @@ static long long split_rows(const PDims& dm, int dtype) {
   if (dtype == CAOTE_BF16) return 256LL * g_sm_count;
   return rows * kMostSplits < most ? rows * kMostSplits : most;
 }
-// Calls with few rows per sequence over pages take the kernels of paged_decode.cuh: up to kFewRows rows of a pair. Single tokens of
-// groups up to 16, or a few drafted tokens of small groups; beyond that the row blocks' padding costs less than more columns would.
-constexpr int kFewRows = 16;
-static bool few_rows(const PDims& dm, int dtype) {
+// Calls with few rows per sequence over pages take the kernels of paged_decode.cuh: single tokens of groups up to 16, a few drafted
+// tokens of small groups. With the weights wanted, up to 16 rows of a pair, since every row's logits are kept in the workspace
+// (4 bytes per slot and row); without, up to 32.
+constexpr int kFewRowsMass = 16, kFewRows = 32;
+static bool few_rows(const PDims& dm, int dtype, bool mass) {
   const long long tiles = (((long long)dm.max_pages << dm.page_shift) + few::kTok - 1) / few::kTok * dm.B * dm.Hkv;
-  return dtype == CAOTE_BF16 && dm.max_pages > 0 && dm.scale > 0.f && (long long)dm.max_new * dm.G <= kFewRows && tiles < (1LL << 31);
+  return dtype == CAOTE_BF16 && dm.max_pages > 0 && dm.scale > 0.f && (long long)dm.max_new * dm.G <= (mass ? kFewRowsMass : kFewRows) &&
+         tiles < (1LL << 31) && dm.B * dm.Hkv <= 65535;
 }
 static int few_workers() { return g_sm_count * few::kWarps; }
 static size_t carve(const PDims& dm, int dtype, char* base, Scratch* out) {
@@ -100,12 +102,12 @@ static size_t carve(const PDims& dm, int dtype, char* base, Scratch* out) {
     // (a workspace for more rows per sequence serves calls with fewer: sized for the most rows that come here)
     off = 0;
     const long long r = (long long)dm.max_new * dm.G;
-    const size_t rows = r > 8 ? kFewRows : 8, pairs = (size_t)dm.B * dm.Hkv;
+    const size_t rows = r > kFewRows ? kFewRows : (size_t)(r + 7) / 8 * 8, pairs = (size_t)dm.B * dm.Hkv;
     s.rec.slots = dm.max_pages << dm.page_shift;
     s.rec.plan = reinterpret_cast<int*>(take((size_t)dm.B + 2));
     s.rec.stat = take((pairs + few_workers()) * rows);
     s.rec.o = take((pairs + few_workers()) * rows * dm.D);
-    s.rec.logits = take(pairs * s.rec.slots * rows);
+    s.rec.logits = take(pairs * s.rec.slots * (rows > kFewRowsMass ? kFewRowsMass : rows));
     if (off > most) most = off;
   }
   if (out) *out = s;
@@ -217,7 +219,7 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
                           sc.opart, sc.lpart, sc.notes, g_sm_count, most_splits, status + kItemCounter, status));
   if (most_splits > 1)
     CAOTE_LAUNCH("paged_combine", st,
-                 launch_pdl(tcore::combine_kernel<D>, dim3(g_sm_count, 8), dim3(256), 0, st, dm, sq, (__nv_bfloat16*)o, lse, sc.lse2,
+                 launch_pdl(tcore::combine_kernel<D>, dim3((unsigned)(items < g_sm_count ? items : g_sm_count - 1), 8), dim3(256), 0, st, dm, sq, (__nv_bfloat16*)o, lse, sc.lse2,
                             (const float*)sc.opart, (const float*)sc.lpart, (const tcore::SplitNote*)sc.notes));
   if (mass)
     CAOTE_LAUNCH("paged_mass_kernel", st,
@@ -259,10 +261,17 @@ static int attend(const caote_paged_params_t* p, const PDims& dm, const Seqs& sq
     return dm.D == 128 ? attend_generic<float, 128, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st)
                        : attend_generic<float, 64, kPaged>(dm, sq, q, K, V, o, lse, mass, ws, st);
   if constexpr (kPaged) {
-    if (few_rows(dm, p->dtype) && dm.B * dm.Hkv <= 65535) {
-      const bool one = dm.max_new * dm.G <= 8;
-      if (dm.D == 128) return one ? attend_few<128, 1>(dm, sq, q, K, V, o, lse, mass, ws, st) : attend_few<128, 2>(dm, sq, q, K, V, o, lse, mass, ws, st);
-      return one ? attend_few<64, 1>(dm, sq, q, K, V, o, lse, mass, ws, st) : attend_few<64, 2>(dm, sq, q, K, V, o, lse, mass, ws, st);
+    if (few_rows(dm, p->dtype, mass != nullptr)) {
+      auto run = [&](auto d) -> int {
+        constexpr int D = decltype(d)::value;
+        switch ((dm.max_new * dm.G + 7) / 8) {
+          case 1: return attend_few<D, 1>(dm, sq, q, K, V, o, lse, mass, ws, st);
+          case 2: return attend_few<D, 2>(dm, sq, q, K, V, o, lse, mass, ws, st);
+          case 3: return attend_few<D, 3>(dm, sq, q, K, V, o, lse, mass, ws, st);
+          default: return attend_few<D, 4>(dm, sq, q, K, V, o, lse, mass, ws, st);
+        }
+      };
+      return dm.D == 128 ? run(std::integral_constant<int, 128>{}) : run(std::integral_constant<int, 64>{});
     }
   }
   if (dm.scale > 0.f)  // (the tensor-core kernels take the largest product for the largest logit)

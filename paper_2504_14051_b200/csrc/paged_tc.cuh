@@ -107,6 +107,11 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               PDims dm, Seqs sq, int box, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ lse2,
               float* __restrict__ opart, float* __restrict__ lpart, SplitNote* __restrict__ notes, int sms, int most_splits, int* next_item, int* status) {
   constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16, kKS = kKStages<D>, kVS = kVStages<D>;
+  if (threadIdx.x == 0) {
+    ptx::prefetch_map(&tmQ);
+    ptx::prefetch_map(&tmK);
+    ptx::prefetch_map(&tmV);
+  }
   ptx::pdl_wait();
   ptx::pdl_trigger();
   extern __shared__ char smem_raw[];
@@ -136,7 +141,7 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     if (lane == 0) {
       *where = Where{there ? p.b : -1, (p.blocks - 1 - p.block) * 2 * tok, item % dm.Hkv, x < 0 ? 0 : x % c.splits, x < 0 ? 1 : c.splits, x, p.s};
       if (blockIdx.x == 0) {
-        *next_item = 0;  // (for the mass kernel)
+        *next_item = sms;  // (for the mass kernel, whose CTAs begin with items of their own number)
         notes[0] = make_int4(c.splits > 1 ? c.items - c.whole : 0, c.splits, 0, 0);
       }
     }
@@ -421,33 +426,37 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         }
       }
     } else {
-      // [x][block][half of the channels][row], as they lie in shared memory: the threads of either half in turn
+      // [x][block][quarter of the channels][row], pieces as they lie in shared memory: a warp has 32 rows x two quarters
       const size_t slot = (size_t)where->x * (2 * kTile) + i * kTile;
       if (valid && hf == 0) lpart[slot + row] = stat;
       if (c > 0) {
-#pragma unroll 1
-        for (int turn = 0; turn < 2; ++turn) {
-          if (turn == hf) {
+        constexpr int kQ = D / 4, kPieces = kQ / 4;
+        char* quarter = mine + hf * (kTB / 8);
 #pragma unroll
-            for (int cc = 0; cc < D / 64; ++cc) {
-              float v[32];
-              tmem_ld32(t_o + cc * 32, v);
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                *reinterpret_cast<float4*>(place(lane, cc * 8 + e)) = make_float4(v[4 * e] * inv, v[4 * e + 1] * inv, v[4 * e + 2] * inv, v[4 * e + 3] * inv);
-            }
-            ptx::fence_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              ptx::bulk_store(opart + (slot * 2 + hf * kTile + (warp & 3) * 32) * (D / 2), mine, kTB / 4);
-              ptx::bulk_commit();
-              ptx::bulk_wait_read();
-            }
+        for (int e0 = 0; e0 < 2; ++e0) {
+          if (e0 == 1) {
+            if (lane == 0) ptx::bulk_wait_read();
             __syncwarp();
           }
-          asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+#pragma unroll
+          for (int cc = 0; cc < kQ / 16; ++cc) {
+            uint32_t v[16];
+            tmem_ld16_issue(t_o + e0 * kQ + cc * 16, v);
+            tmem_ld16_wait(v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<float4*>(quarter + lane * (kQ * 4) + (((cc * 4 + e) ^ (lane & (kPieces - 1))) << 4)) =
+                  make_float4(__uint_as_float(v[4 * e]) * inv, __uint_as_float(v[4 * e + 1]) * inv, __uint_as_float(v[4 * e + 2]) * inv,
+                              __uint_as_float(v[4 * e + 3]) * inv);
+          }
+          ptx::fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            ptx::bulk_store(opart + (slot * 4 + (hf * 2 + e0) * kTile + (warp & 3) * 32) * kQ, quarter, 32 * kQ * 4);
+            ptx::bulk_commit();
+          }
         }
-        ptx::bulk_wait();
+        if (lane == 0) ptx::bulk_wait();
       }
     }
   }
@@ -457,63 +466,71 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
-// o = sum_s o_s 2^(lse_s - lse) over the splits of the rows of split items. grid = (SMs, 8): a CTA has 32 rows of an item, four per
-// warp.
+// o = sum_s o_s 2^(lse_s - lse) over the splits of the rows of split items. grid = (most split items, 8): a CTA has 32 rows of an item,
+// four per warp; a lane has 16 bytes of a row's partial output (head_dim 64: of every other split's).
 template <int D>
 __global__ void __launch_bounds__(256)
 combine_kernel(PDims dm, Seqs sq, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ lse2,
                const float* __restrict__ opart, const float* __restrict__ lpart, const SplitNote* __restrict__ notes) {
   ptx::pdl_wait();
   ptx::pdl_trigger();
-  constexpr int CPL = D / 32, kR = 4;
+  constexpr int kR = 4, kLanes = D / 4, kStep = 32 / kLanes, kQ = D / 4, kPieces = kQ / 4;
   const int tok = kTile / dm.G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const SplitNote all = notes[0], it = notes[1 + blockIdx.x];
   if ((int)blockIdx.x >= all.x || it.w == 1) return;
   const int t0 = sq.cu[it.x], m = sq.cu[it.x + 1] - t0, i0 = it.y, h = it.z, count = it.w;
   const int local0 = blockIdx.y * 32 + warp * kR, i = local0 / kTile, row0 = local0 % kTile;
-  const size_t slot = (size_t)blockIdx.x * all.y * (2 * kTile) + local0;
-  // channel k * 32 + lane of row `row0 + e` as attend_kernel left it
-  auto part_at = [&](int sp, int e, int k) {
-    const int ch = k * 32 + lane, row = row0 + e, in_half = ch % (D / 2);
-    const size_t base = ((size_t)blockIdx.x * all.y + sp) * (2 * kTile) + i * kTile;
-    return ((base * 2 + (ch / (D / 2)) * kTile + row) * (D / 2)) + ((((in_half >> 2) ^ (row & 7)) << 2) | (in_half & 3));
-  };
+  const size_t base = (size_t)blockIdx.x * all.y * (2 * kTile) + i * kTile;  // of split 0
+  // this lane's four channels, and where they lie for row r: in quarter `qu`, piece `piece` of the row
+  const int ch = lane % kLanes * 4, qu = ch / kQ, piece = ch % kQ / 4, sp0 = lane / kLanes;
   float mine[kR];
 #pragma unroll
   for (int e = 0; e < kR; ++e) {
     const bool there = row0 + e < tok * dm.G && i0 + i * tok + (row0 + e) / dm.G < m;
-    mine[e] = there && lane < count ? lpart[slot + (size_t)lane * (2 * kTile) + e] : -INFINITY;
+    mine[e] = there && lane < count ? lpart[base + (size_t)lane * (2 * kTile) + row0 + e] : -INFINITY;
   }
-  float stat[kR], v[kR][CPL];
+  float stat[kR];
+  float4 v[kR];
 #pragma unroll
   for (int e = 0; e < kR; ++e) {
     const float top = warp_max(mine[e]);
     mine[e] = top == -INFINITY ? 0.f : ptx::fast_exp2(mine[e] - top);
     const float sum = warp_sum(mine[e]);
     stat[e] = top + __log2f(sum);
-    mine[e] *= 1.f / sum;
-#pragma unroll
-    for (int k = 0; k < CPL; ++k) v[e][k] = 0.f;
+    mine[e] = sum > 0.f ? mine[e] / sum : 0.f;
+    v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-#pragma unroll 2
-  for (int sp = 0; sp < count; ++sp) {
+#pragma unroll 4
+  for (int s0 = 0; s0 < count; s0 += kStep) {
+    const int sp = s0 + sp0;
 #pragma unroll
     for (int e = 0; e < kR; ++e) {
-      const float w = __shfl_sync(0xffffffffu, mine[e], sp);
-#pragma unroll
-      for (int k = 0; k < CPL; ++k)  // (a split in which the row sees no key has written no output)
-        v[e][k] = fmaf(w, w > 0.f ? opart[part_at(sp, e, k)] : 0.f, v[e][k]);
+      const float w = __shfl_sync(0xffffffffu, mine[e], min(sp, 31));  // (0 behind the last split)
+      if (w > 0.f) {  // (a split in which the row sees no key has written no output)
+        const int row = row0 + e;
+        const float4 x = *reinterpret_cast<const float4*>(
+            opart + ((base + (size_t)sp * (2 * kTile)) * 4 + qu * kTile + row) * kQ + ((piece ^ (row & (kPieces - 1))) << 2));
+        v[e].x = fmaf(w, x.x, v[e].x);
+        v[e].y = fmaf(w, x.y, v[e].y);
+        v[e].z = fmaf(w, x.z, v[e].z);
+        v[e].w = fmaf(w, x.w, v[e].w);
+      }
     }
   }
   Seq s;
   s.t0 = t0;
 #pragma unroll
   for (int e = 0; e < kR; ++e) {
+    if (kStep == 2) {
+      v[e].x += __shfl_xor_sync(0xffffffffu, v[e].x, 16);
+      v[e].y += __shfl_xor_sync(0xffffffffu, v[e].y, 16);
+      v[e].z += __shfl_xor_sync(0xffffffffu, v[e].z, 16);
+      v[e].w += __shfl_xor_sync(0xffffffffu, v[e].w, 16);
+    }
     const int tkn = i0 + i * tok + (row0 + e) / dm.G;
     if (row0 + e >= tok * dm.G || tkn >= m) continue;
     const size_t at = (size_t)(t0 + tkn) * dm.Hq + h * dm.G + (row0 + e) % dm.G;
-#pragma unroll
-    for (int k = 0; k < CPL; ++k) o[at * D + k * 32 + lane] = __float2bfloat16_rn(v[e][k]);
+    if (lane < kLanes) *reinterpret_cast<uint2*>(o + at * D + ch) = make_uint2(pack_bf16(v[e].x, v[e].y), pack_bf16(v[e].z, v[e].w));
     if (lane == 0) {
       lse2[stat_at(dm, s, h, (i0 + i * tok) * dm.G + row0 + e)] = stat[e];
       if (lse) lse[at] = stat[e] * kLn2;
@@ -560,12 +577,16 @@ struct Item {
   Seq s;
 };
 
-// grid: one CTA per SM. next_item: 0 at the start (the attention pass leaves it so).
+// grid: one CTA per SM. next_item: their number at the start (the attention pass leaves it so).
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kMassThreads, 1)
 mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, PDims dm, Seqs sq, int box,
             const float* __restrict__ lse2, float* __restrict__ mass, int* next_item, int* status) {
   constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16, kQS = kQStages<D>;
+  if (threadIdx.x == 0) {
+    ptx::prefetch_map(&tmQ);
+    ptx::prefetch_map(&tmK);
+  }
   ptx::pdl_wait();
   ptx::pdl_trigger();
   extern __shared__ char smem_raw[];
@@ -582,63 +603,72 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   __shared__ Item items[2];
 
   const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
-  if (tid == 0) {
+  const int tok = kTile / dm.G;
+  // the item of number `it`, its K tiles' pages (this lane's) and boxes; the warp of the items
+  auto what = [](const Seq& x) { return x.m > 0 ? x.n : 0; };
+  struct Next { Item x; int id[2], boxes[2]; } nx;
+  Scan seqs;
+  auto find = [&](int it) {
+    // A prompt's first keys are seen by most rows: the heads take turns, so that what comes last is short. (Head by head the
+    // last head's first keys come late: 2.84 instead of 1.4 ms, 64/8 heads, prompts of 7 428 and 8 956 tokens.)
+    Place p;
+    nx.id[0] = nx.id[1] = nx.boxes[0] = nx.boxes[1] = 0;
+    if (!find_block(dm, sq, kKeys, it / dm.Hkv, what, seqs, p)) {
+      nx.x.b = -1;
+      return;
+    }
+    nx.x.b = p.b;
+    nx.x.h = it % dm.Hkv;
+    nx.x.s = p.s;
+    nx.x.j0 = p.block * kKeys;
+    nx.x.rb0 = max(0, nx.x.j0 - (p.s.n - p.s.m)) / tok;
+    nx.x.blocks = (p.s.m + tok - 1) / tok - nx.x.rb0;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+      if (nx.x.j0 + kk * kTile < p.s.n) {
+        nx.id[kk] = page_of<kPaged>(dm, sq, p.b, p.s.n, nx.x.j0 + kk * kTile, box, status);
+        nx.boxes[kk] = boxes_of<kPaged>(p.s, nx.x.j0 + kk * kTile, box);
+      }
+  };
+  // the set-up's parts side by side
+  if (warp == 17) {
+    seqs = scan(dm, sq, 0, kKeys, what, nullptr);
+    find(blockIdx.x);
+  } else if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+  } else if (tid == 0) {
     for (int i = 0; i < kBars1; ++i) mbar_init(&bars[i], 1);
     for (int i = 0; i < 2 + kStatStages; ++i) mbar_init(&s_free[i], kKeyThreads / 32);
     // an item's place comes free when the key warps, the Q copies, the statistics and the products are done with it
     for (int i = 0; i < 2; ++i) mbar_init(&item_free[i], kKeyThreads / 32 + 3);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 0) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;  // S^T of key tile kk, buffer buf: columns [kk * 256 + buf * 128, + 128)
-  const int tok = kTile / dm.G;
 
   if (warp == 17) {
     // =============================== items and their K (the warp) ===============================
-    auto what = [](const Seq& x) { return x.m > 0 ? x.n : 0; };
-    const Scan seqs = scan(dm, sq, 0, kKeys, what, nullptr);
     for (int c = 0;; ++c) {
       const int buf = c & 1;
-      int it = 0;
-      if (lane == 0) it = atomicAdd(next_item, 1);
-      it = __shfl_sync(0xffffffffu, it, 0);
-      Item x;
-      // A prompt's first keys are seen by most rows: the heads take turns, so that what comes last is short. (Head by head the
-      // last head's first keys come late: 2.84 instead of 1.4 ms, 64/8 heads, prompts of 7 428 and 8 956 tokens.)
-      Place p;
-      if (find_block(dm, sq, kKeys, it / dm.Hkv, what, seqs, p)) {
-        x.b = p.b;
-        x.h = it % dm.Hkv;
-        x.s = p.s;
-        x.j0 = p.block * kKeys;
-        x.rb0 = max(0, x.j0 - (x.s.n - x.s.m)) / tok;
-        x.blocks = (x.s.m + tok - 1) / tok - x.rb0;
-      } else {
-        x.b = -1;
+      if (c > 0) {
+        int it = 0;
+        if (lane == 0) it = atomicAdd(next_item, 1);
+        find(__shfl_sync(0xffffffffu, it, 0));
       }
-      int id[2] = {0, 0}, boxes[2] = {0, 0};
-      if (x.b >= 0) {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-          if (x.j0 + kk * kTile < x.s.n) {
-            id[kk] = page_of<kPaged>(dm, sq, x.b, x.s.n, x.j0 + kk * kTile, box, status);
-            boxes[kk] = boxes_of<kPaged>(x.s, x.j0 + kk * kTile, box);
-          }
-      }
+      const Item& x = nx.x;
       if (c >= 2) mbar_wait_idle(&item_free[buf], ((c >> 1) - 1) & 1, status);
       if (lane == 0) {
         items[buf] = x;
-        if (x.b >= 0) mbar_expect_tx(&k_bar[buf], (boxes[0] + boxes[1]) * box * D * 2);  // (also says that the item is there)
+        if (x.b >= 0) mbar_expect_tx(&k_bar[buf], (nx.boxes[0] + nx.boxes[1]) * box * D * 2);  // (also says that the item is there)
         else mbar_arrive(&k_bar[buf]);
       }
       __syncwarp();
       if (x.b < 0) break;
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
-        if (boxes[kk] > 0) copy_keys<D, kPaged>(dm, &tmK, x.s, x.h, x.j0 + kk * kTile, box, id[kk], Ks + (2 * buf + kk) * kTB, &k_bar[buf]);
+        if (nx.boxes[kk] > 0) copy_keys<D, kPaged>(dm, &tmK, x.s, x.h, x.j0 + kk * kTile, box, nx.id[kk], Ks + (2 * buf + kk) * kTB, &k_bar[buf]);
     }
   } else if (warp == 18) {
     // =============================== copies of the Q blocks (one lane) ===============================
@@ -812,7 +842,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 0) tmem_dealloc(tmem, 512);
+  if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
 }  // namespace tcore
