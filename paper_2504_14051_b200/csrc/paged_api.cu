@@ -321,10 +321,10 @@ int caote_paged_append(const caote_paged_params_t* p, void* K, void* V, float* m
   const paged::PDims dm = paged::make_dims(p, true, 0, kv_stride);
   const int e = p->dtype == CAOTE_BF16 ? 2 : 4, row_bytes = dm.D * e;
   const long long pieces = (long long)dm.T * dm.Hkv * 2 * (row_bytes / 16);
-  long long ctas = (pieces + 255) / 256;
+  long long ctas = (pieces + paged::kAppendThreads - 1) / paged::kAppendThreads;
   if (ctas > 8LL * g_sm_count) ctas = 8LL * g_sm_count;
   CAOTE_LAUNCH("paged_append_kernel", (cudaStream_t)stream,
-               launch_pdl(paged::append_kernel, dim3((unsigned)ctas), dim3(256), 0, (cudaStream_t)stream, dm,
+               launch_pdl(paged::append_kernel, dim3((unsigned)ctas), dim3(paged::kAppendThreads), 0, (cudaStream_t)stream, dm,
                           paged::Seqs{cu, len, page_table}, row_bytes, dm.kv_stride * e, (char*)K, (char*)V, mass, pos, len, n_seen,
                           (const char*)k_new, (const char*)v_new, mass_new, (int*)workspace, (int*)workspace + 4));
   return CAOTE_OK;
@@ -352,16 +352,25 @@ int caote_paged_evict(const caote_paged_params_t* p, void* K, void* V, float* ma
     return CAOTE_ERR_INVALID_ARG;
   if (!paged::params_supported(p)) return CAOTE_ERR_UNSUPPORTED;
   if (sinks < 0 || recent < 0 || max_evict < 1 || !aligned(K, 16) || !aligned(V, 16)) return CAOTE_ERR_INVALID_ARG;
-  if ((long long)p->batch * p->n_kv_heads >= (1LL << 31)) return CAOTE_ERR_INVALID_ARG;
+  if ((long long)p->batch * p->n_kv_heads >= (1LL << 28)) return CAOTE_ERR_INVALID_ARG;
   if (!paged::workspace_ok(workspace, workspace_bytes, kHeaderBytes)) return CAOTE_ERR_INVALID_ARG;
   int rc = check_device();
   if (rc) return rc;
   const paged::PDims dm = paged::make_dims(p, true, 0, 0);
   const int row_bytes = dm.D * (p->dtype == CAOTE_BF16 ? 2 : 4);
+  // One token per pair: a cluster per sequence, whose first CTA moves the length on. Several: up to four CTAs per pair while they
+  // all run at once, for the rows that move (64 pairs, 512 rows each: 9 us of moves on single CTAs, half of it on two).
+  const bool by_sequence = max_evict == 1 && dm.Hkv <= 8;
+  int c = by_sequence ? dm.Hkv : 1;
+  if (!by_sequence && max_evict >= 64) {
+    refresh_sm_count();
+    while (c < 4 && (long long)dm.B * dm.Hkv * 2 * c <= g_sm_count) c *= 2;
+  }
   CAOTE_LAUNCH("paged_evict_kernel", (cudaStream_t)stream,
-               launch_pdl(paged::evict_kernel, dim3(dm.B * dm.Hkv), dim3(paged::kEvictThreads), 0, (cudaStream_t)stream, dm,
-                          paged::Seqs{nullptr, len, page_table}, paged::Pool{(char*)K, (char*)V, mass, pos}, row_bytes, len, n_seen, budget,
-                          sinks, recent, evict_idx, max_evict, n_evict, (int*)workspace, (int*)workspace + 4));
+               launch_pdl_clusters(paged::evict_kernel, dim3((unsigned)(dm.B * dm.Hkv * (by_sequence ? 1 : c))), dim3(paged::kEvictThreads), 0, c,
+                                   (cudaStream_t)stream, dm, paged::Seqs{nullptr, len, page_table}, paged::Pool{(char*)K, (char*)V, mass, pos},
+                                   row_bytes, len, n_seen, budget, sinks, recent, evict_idx, max_evict, n_evict, by_sequence, (int*)workspace,
+                                   (int*)workspace + 4));
   return CAOTE_OK;
 }
 

@@ -5,8 +5,8 @@
 // sequence. The survivors among the last k slots move into the holes below the new length, so that a pair's tokens stay in its
 // first slots and whole pages come free behind them.
 //
-// What bounds them: chains of dependent reads (length, page table, weights, picks, rows), a CTA per pair; the traffic is 8 bytes
-// per token and four rows per evicted one.
+// What bounds them: chains of dependent reads (length, page table, weights, picks, rows); the traffic is 8 bytes per token and four
+// rows per evicted one.
 #pragma once
 
 #include "paged_common.cuh"
@@ -19,64 +19,76 @@ namespace paged {
 constexpr int kEvictThreads = sel::kSelThreads;
 constexpr unsigned kSheltered = 0xffffffffu;  // as the score bits of a sheltered token: behind every other
 
-// Whether all pages of slots [from, to) lie in the pool; for a whole CTA, the same result in every thread.
-__device__ __forceinline__ bool pages_ok(const PDims& dm, const int* __restrict__ table, int from, int to) {
-  bool ok = true;
-  for (int p = (from >> dm.page_shift) + threadIdx.x; p <= (to - 1) >> dm.page_shift; p += blockDim.x)
-    ok = ok && (unsigned)__ldg(table + p) < (unsigned)dm.n_pages;
-  return __syncthreads_and(ok) != 0;
-}
-
-// New rows into the pages: a thread per 16 bytes of a K or V row, grid-stride over (token, KV head, K or V, piece). The CTA that
-// finishes last moves the lengths on; a sequence that does not fit, or one of whose pages is none, keeps its length.
-__global__ void __launch_bounds__(256)
+// New rows into the pages: a thread per 16 bytes of a K or V row, the pieces of a token side by side. The CTA that finishes last moves
+// the lengths on; a sequence that does not fit, or one of whose pages is none, keeps its length.
+constexpr int kAppendThreads = 256, kSharedStarts = 1024;
+__global__ void __launch_bounds__(kAppendThreads)
 append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __restrict__ K, char* __restrict__ V,
               float* __restrict__ mass, int* __restrict__ pos, int* __restrict__ len, int* __restrict__ n_seen,
               const char* __restrict__ k_new, const char* __restrict__ v_new, const float* __restrict__ mass_new, int* status,
               int* ticket) {
   ptx::pdl_wait();
   ptx::pdl_trigger();
+  __shared__ int s_cu[kSharedStarts + 1];
+  const int tid = threadIdx.x;
+  // (a search of dependent reads: from shared memory where the starts fit)
+  const bool in_smem = dm.B <= kSharedStarts;
+  if (in_smem) {
+    for (int b = tid; b <= dm.B; b += kAppendThreads) s_cu[b] = sq.cu[b];
+    __syncthreads();
+  }
+  auto start = [&](int b) { return in_smem ? s_cu[b] : __ldg(sq.cu + b); };
   const int pieces = row_bytes / 16, per_token = dm.Hkv * 2 * pieces;
-  const long long total = (long long)dm.T * per_token;
+  const int at_once = per_token < kAppendThreads ? kAppendThreads / per_token : 1;  // tokens
   const long long cap = (long long)dm.max_pages << dm.page_shift;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
-    const int t = (int)(i / per_token), rest = (int)(i % per_token);
-    const int h = rest / (2 * pieces), which = rest / pieces & 1, c = rest % pieces;
-    int lo = 0, hi = dm.B;  // the sequence of token t
+  const int sub = per_token < kAppendThreads ? tid / per_token : 0, rest0 = tid - sub * per_token;
+  for (int t = blockIdx.x * at_once + sub; t < dm.T && sub < at_once; t += gridDim.x * at_once) {
+    auto source = [&](int rest) {
+      const int h = rest / (2 * pieces);
+      return *reinterpret_cast<const uint4*>((rest / pieces & 1 ? v_new : k_new) + (size_t)t * src_stride + (size_t)h * row_bytes + rest % pieces * 16);
+    };
+    uint4 x = make_uint4(0u, 0u, 0u, 0u);  // (on its way while the token's place is looked up)
+    if (rest0 < per_token) x = source(rest0);
+    int lo = 0, hi = dm.B;  // the sequence of token t: the last one that begins at or before it
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (__ldg(sq.cu + mid) <= t) lo = mid; else hi = mid;
+      if (start(mid) <= t) lo = mid; else hi = mid;
     }
-    const int t0 = __ldg(sq.cu + lo), t1 = __ldg(sq.cu + lo + 1), n = len[lo];
+    const int t0 = start(lo), t1 = start(lo + 1), n = len[lo], seen = n_seen ? n_seen[lo] : n;
     if (t < t0 || t >= t1 || t1 > dm.T || t0 < 0 || t1 - t0 > dm.max_new || n < 0 || n + (long long)(t1 - t0) > cap) continue;
     const int j = n + t - t0;
     const int page = __ldg(sq.table + (size_t)lo * dm.max_pages + (j >> dm.page_shift));
     if ((unsigned)page >= (unsigned)dm.n_pages) continue;
-    const size_t at = (((size_t)page * dm.Hkv + h) << dm.page_shift) + (j & ((1 << dm.page_shift) - 1));
-    const char* src = (which ? v_new : k_new) + (size_t)t * src_stride + (size_t)h * row_bytes + c * 16;
-    *reinterpret_cast<uint4*>((which ? V : K) + at * row_bytes + c * 16) = *reinterpret_cast<const uint4*>(src);
-    if (which == 0 && c == 0) {
-      if (mass) mass[at] = mass_new ? mass_new[(size_t)t * dm.Hkv + h] : 0.f;
-      if (pos) pos[at] = (n_seen ? n_seen[lo] : n) + t - t0;
+    const size_t row0 = ((size_t)page * dm.Hkv << dm.page_shift) + (j & ((1 << dm.page_shift) - 1));  // of head 0
+    for (int rest = rest0; rest < per_token; rest += kAppendThreads) {
+      const int h = rest / (2 * pieces), which = rest / pieces & 1, c = rest % pieces;
+      const size_t at = row0 + ((size_t)h << dm.page_shift);
+      if (rest != rest0) x = source(rest);
+      *reinterpret_cast<uint4*>((which ? V : K) + at * row_bytes + c * 16) = x;
+      if (which == 0 && c == 0) {
+        if (mass) mass[at] = mass_new ? mass_new[(size_t)t * dm.Hkv + h] : 0.f;
+        if (pos) pos[at] = seen + t - t0;
+      }
     }
   }
   __shared__ int s_last;
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     __threadfence();
     s_last = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
   }
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  for (int b = threadIdx.x; b < dm.B; b += blockDim.x) {
-    const int t0 = sq.cu[b], t1 = sq.cu[b + 1], m = t1 - t0, n = len[b];
+  for (int b = tid; b < dm.B; b += kAppendThreads) {
+    const int t0 = start(b), t1 = start(b + 1), m = t1 - t0, n = len[b];
     if (t0 < 0 || t1 < t0 || t1 > dm.T || m > dm.max_new || n < 0) {
       set_status(status, CAOTE_ERR_BAD_LENGTH);
     } else if (n + (long long)m > cap) {
       set_status(status, CAOTE_ERR_OVERFLOW);
     } else if (m > 0) {
       bool ok = true;
+#pragma unroll 4
       for (int p = n >> dm.page_shift; p <= (n + m - 1) >> dm.page_shift; ++p)
         ok = ok && (unsigned)__ldg(sq.table + (size_t)b * dm.max_pages + p) < (unsigned)dm.n_pages;
       if (!ok) {
@@ -87,26 +99,40 @@ append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __re
       }
     }
   }
-  if (threadIdx.x == 0) *ticket = 0;
+  if (tid == 0) *ticket = 0;
 }
 
+constexpr int kMoves = 512;   // rows whose moves are worked out at a time
 struct Pool {
   char *K, *V;
   float* mass;
   int* pos;
 };
 
-// One CTA per (sequence, KV head) pair: selection, compaction; the CTA that finishes last moves the lengths.
+// The position of slot j of a pair.
+struct Positions {
+  const int *table, *pos;
+  int Hkv, h, shift, n_pages;
+  __device__ __noinline__ unsigned operator()(int j) const {
+    const int page = __ldg(table + (j >> shift));
+    return (unsigned)page < (unsigned)n_pages ? (unsigned)pos[(((size_t)page * Hkv + h) << shift) + (j & ((1 << shift) - 1))] : 0u;
+  }
+};
+
+// Selection and compaction. grid = (sequence, KV head) pairs x C in clusters:
+//   by_sequence (one token goes per pair at most): a cluster is a sequence, a CTA a pair; rank 0 moves the length on.
+//   else: a cluster is a pair. Rank 0 selects, all of its CTAs move rows; the CTA that finishes last moves the lengths on.
 __global__ void __launch_bounds__(kEvictThreads)
 evict_kernel(PDims dm, Seqs sq, Pool pool, int row_bytes, int* __restrict__ len, const int* __restrict__ n_seen,
              const int* __restrict__ budget, int sinks, int recent, int* __restrict__ evict_idx, int max_evict,
-             int* __restrict__ n_evict, int* status, int* ticket) {
+             int* __restrict__ n_evict, bool by_sequence, int* status, int* ticket) {
   ptx::pdl_wait();
   ptx::pdl_trigger();
   __shared__ int s_picks[sel::kMaxSharedPicks];
-  __shared__ unsigned long long s_key[kEvictThreads / 32];
-  __shared__ int s_slot[kEvictThreads / 32];
-  const int b = blockIdx.x / dm.Hkv, h = blockIdx.x % dm.Hkv;
+  __shared__ unsigned s_min[3][kEvictThreads / 32];
+  __shared__ int2 s_moves[kMoves];
+  const int C = by_sequence ? 1 : (int)ptx::cluster_nctarank(), rank = by_sequence ? 0 : (int)ptx::cluster_ctarank();
+  const int pair = blockIdx.x / C, b = pair / dm.Hkv, h = pair % dm.Hkv;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int* table = sq.table + (size_t)b * dm.max_pages;
   const int n = len[b], seen = n_seen[b];
@@ -120,83 +146,202 @@ evict_kernel(PDims dm, Seqs sq, Pool pool, int row_bytes, int* __restrict__ len,
     if (tid == 0) set_status(status, CAOTE_ERR_OVERFLOW);
     k = 0;
   }
-  if (k > 0 && !pages_ok(dm, table, 0, n)) {  // (every pair of the sequence comes to the same answer)
-    if (tid == 0) set_status(status, CAOTE_ERR_BAD_PAGE);
-    k = 0;
-  }
-  if (h == 0 && tid == 0) n_evict[b] = k;
-  if (k > 0) {
-    const int shift = dm.page_shift, low = (1 << shift) - 1, Hkv = dm.Hkv;
-    auto row = [=](int j) { return (((size_t)__ldg(table + (j >> shift)) * Hkv + h) << shift) + (j & low); };
-    const float* mass = pool.mass;
-    const int* pos = pool.pos;
-    const long long newest = (long long)seen - recent;
-    auto position = [=](int j) { return (unsigned)pos[row(j)]; };
-    auto score = [=](int j) {
-      const size_t at = row(j);
-      const unsigned w = __float_as_uint(mass[at]);
-      const int p = pos[at];
-      return p < sinks || p >= newest ? kSheltered : min(w, kSheltered - 1u);
-    };
-    int* out = evict_idx + (size_t)blockIdx.x * max_evict;
-    const int left = n - k;
-    const int* E;
-    if (k == 1) {
-      unsigned long long best = ~0ull;
-      int best_slot = n;
-      for (int j = tid; j < n; j += kEvictThreads) {
-        const size_t at = row(j);
-        const unsigned w = __float_as_uint(mass[at]);
-        const int p = pos[at];
-        const unsigned long long key = sel::make_key(p < sinks || p >= newest ? kSheltered : min(w, kSheltered - 1u), (unsigned)p);
-        if (key < best || best_slot == n) { best = key; best_slot = j; }
+  const int shift = dm.page_shift, low = (1 << shift) - 1, Hkv = dm.Hkv, n_pages = dm.n_pages;
+  // (a page outside the pool is read as page 0 and remembered: nothing is written then)
+  bool bad = false;
+  auto row = [&](int j) {
+    int page = __ldg(table + (j >> shift));
+    if ((unsigned)page >= (unsigned)n_pages) {
+      bad = true;
+      page = 0;
+    }
+    return (((size_t)page * Hkv + h) << shift) + (j & low);
+  };
+  const float* mass = pool.mass;
+  const int* pos = pool.pos;
+  const long long newest = (long long)seen - recent;
+  auto bits = [&](unsigned w, int p) { return p < sinks || p >= newest ? kSheltered : min(w, kSheltered - 1u); };
+  int* out = evict_idx + (size_t)pair * max_evict;
+  const int left = n - k;
+  if (k == 1) {
+    if (rank == 0) {
+      // the last row, which fills the hole, is on its way while the hole is looked for: warp 0 has K, warp 1 V
+      const bool mover = warp < 2 && lane * 16 < row_bytes;
+      char* rows = warp == 0 ? pool.K : pool.V;
+      const size_t last = warp < 3 ? row(left) : 0;
+      uint4 moved = make_uint4(0u, 0u, 0u, 0u);
+      if (mover) moved = *reinterpret_cast<const uint4*>(rows + last * row_bytes + lane * 16);
+      float last_mass = 0.f;
+      int last_pos = 0;
+      if (warp == 2 && lane == 0) {
+        last_mass = mass[last];
+        last_pos = pos[last];
       }
-      auto reduce = [&]() {
+      unsigned bw = ~0u, bp = ~0u, bs = ~0u;  // the first token so far: score bits, position, slot
+      constexpr int kAtOnce = 8;
+      for (int j0 = tid; j0 < n; j0 += kAtOnce * kEvictThreads) {
+        unsigned w[kAtOnce];
+        int p[kAtOnce];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          const unsigned long long ok = __shfl_xor_sync(0xffffffffu, best, o);
-          const int os = __shfl_xor_sync(0xffffffffu, best_slot, o);
-          if (ok < best || (ok == best && os < best_slot)) { best = ok; best_slot = os; }
+        for (int e = 0; e < kAtOnce; ++e) {
+          const int j = j0 + e * kEvictThreads;
+          w[e] = 0u;
+          p[e] = 0;
+          if (j < n) {
+            const size_t at = row(j);
+            w[e] = __float_as_uint(mass[at]);
+            p[e] = pos[at];
+          }
         }
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+          const int j = j0 + e * kEvictThreads;
+          const unsigned x = bits(w[e], p[e]);
+          if (j < n && (bs == ~0u || x < bw || (x == bw && (unsigned)p[e] < bp))) { bw = x; bp = (unsigned)p[e]; bs = (unsigned)j; }
+        }
+      }
+      // the smallest bits, of these the smallest position, of these the smallest slot
+      auto reduce = [&]() {
+        const unsigned mw = __reduce_min_sync(0xffffffffu, bs == ~0u ? ~0u : bw);
+        const unsigned mp = __reduce_min_sync(0xffffffffu, bs != ~0u && bw == mw ? bp : ~0u);
+        const unsigned ms = __reduce_min_sync(0xffffffffu, bs != ~0u && bw == mw && bp == mp ? bs : ~0u);
+        bw = mw; bp = mp; bs = ms;
       };
       reduce();
-      if (lane == 0) { s_key[warp] = best; s_slot[warp] = best_slot; }
-      __syncthreads();
-      best = s_key[lane];
-      best_slot = s_slot[lane];
-      reduce();
-      if (tid == 0) { s_picks[0] = best_slot; out[0] = best_slot; }
-      E = s_picks;
-    } else {
-      int* picks = k <= sel::kMaxSharedPicks ? s_picks : nullptr;
-      if (n <= 8 * kEvictThreads) sel::select_cached<8>(n, k, score, position, out, picks);
-      else if (n <= sel::kMaxCached * kEvictThreads) sel::select_cached<sel::kMaxCached>(n, k, score, position, out, picks);
-      else sel::select_long(n, k, score, position, out, picks);
-      E = picks ? s_picks : out;
-    }
-    __syncthreads();
-    // the i-th survivor among slots [left, n) moves into the i-th hole below `left`: half a warp per row of up to 256 bytes
-    const int holes = sel::lower_bound(E, k, left);
-    const int glanes = row_bytes <= 256 ? 16 : 32, gl = lane & (glanes - 1);
-    const int group = warp * (32 / glanes) + lane / glanes, groups = (kEvictThreads / 32) * (32 / glanes);
-    for (int t = group; t < k; t += groups) {
-      const int src = left + t, lb = holes + sel::lower_bound(E + holes, k - holes, src);
-      if (lb < k && E[lb] == src) continue;  // goes itself
-      const int dst = E[t - (lb - holes)];
-      const size_t so = row(src), to = row(dst);
-      if (gl * 16 < row_bytes) {
-        const uint4 kr = *reinterpret_cast<const uint4*>(pool.K + so * row_bytes + gl * 16);
-        const uint4 vr = *reinterpret_cast<const uint4*>(pool.V + so * row_bytes + gl * 16);
-        *reinterpret_cast<uint4*>(pool.K + to * row_bytes + gl * 16) = kr;
-        *reinterpret_cast<uint4*>(pool.V + to * row_bytes + gl * 16) = vr;
+      if (lane == 0) { s_min[0][warp] = bw; s_min[1][warp] = bp; s_min[2][warp] = bs; }
+      if (__syncthreads_or(bad)) {
+        if (tid == 0) set_status(status, CAOTE_ERR_BAD_PAGE);
+        k = 0;
+      } else if (warp < 3) {
+        bw = s_min[0][lane];
+        bp = s_min[1][lane];
+        bs = s_min[2][lane];
+        reduce();
+        const size_t hole = row((int)bs);
+        if ((int)bs != left) {
+          if (mover) *reinterpret_cast<uint4*>(rows + hole * row_bytes + lane * 16) = moved;
+          if (warp == 2 && lane == 0) {
+            pool.mass[hole] = last_mass;
+            pool.pos[hole] = last_pos;
+          }
+        }
+        if (tid == 0) out[0] = (int)bs;
       }
-      if (gl == 0) {
-        pool.mass[to] = pool.mass[so];
-        pool.pos[to] = pool.pos[so];
+    }
+    if (!by_sequence) ptx::cluster_sync_all();
+  } else if (k > 0) {
+    if (rank == 0) {
+      // (asked for where weights tie only: kept out of the way of the code that always runs)
+      const Positions position{table, pos, Hkv, h, shift, n_pages};
+      // half a dozen tokens' pages, then all of their weights and positions, are on their way at a time
+      auto scores = [&](int first, int count, auto& v) {
+        constexpr int kC = (int)(sizeof(v) / sizeof(v[0])), kAtOnce = kC % 6 == 0 ? 6 : 8;
+        static_assert(kC % kAtOnce == 0, "");
+#pragma unroll
+        for (int i0 = 0; i0 < kC; i0 += kAtOnce) {
+          size_t at[kAtOnce];
+          int p[kAtOnce];
+#pragma unroll
+          for (int e = 0; e < kAtOnce; ++e) {
+            const int j = first + (i0 + e) * kEvictThreads;
+            at[e] = row(j < count ? j : 0);
+          }
+#pragma unroll
+          for (int e = 0; e < kAtOnce; ++e) {
+            v[i0 + e] = __float_as_uint(mass[at[e]]);
+            p[e] = pos[at[e]];
+          }
+#pragma unroll
+          for (int e = 0; e < kAtOnce; ++e) v[i0 + e] = bits(v[i0 + e], p[e]);
+        }
+      };
+      int* picks = k <= sel::kMaxSharedPicks ? s_picks : nullptr;
+      if (n <= 8 * kEvictThreads) sel::select_cached<8, true>(n, k, scores, position, out, picks);
+      else if (n <= 18 * kEvictThreads) sel::select_cached<18, true>(n, k, scores, position, out, picks);
+      else if (n <= sel::kMaxCached * kEvictThreads) sel::select_cached<sel::kMaxCached, true>(n, k, scores, position, out, picks);
+      else {
+        // (by value, not by reference: that would put what the lambdas above refer to on the stack for good)
+        for (int q = tid; q <= (n - 1) >> shift; q += kEvictThreads) bad = bad || (unsigned)__ldg(table + q) >= (unsigned)n_pages;
+        const size_t rows = ((size_t)n_pages * Hkv) << shift;
+        auto row_v = [=](int j) {
+          const size_t at = (((size_t)(unsigned)__ldg(table + (j >> shift)) * Hkv + h) << shift) + (j & low);
+          return at < rows ? at : 0;
+        };
+        auto position_v = [=](int j) { return (unsigned)pos[row_v(j)]; };
+        auto score_v = [=](int j) {
+          const size_t at = row_v(j);
+          const int q = pos[at];
+          return q < sinks || q >= newest ? kSheltered : min(__float_as_uint(mass[at]), kSheltered - 1u);
+        };
+        sel::select_long(n, k, score_v, position_v, out, picks);
+      }
+    } else {
+      for (int q = tid; q <= (n - 1) >> shift; q += kEvictThreads) bad = bad || (unsigned)__ldg(table + q) >= (unsigned)n_pages;
+    }
+    // (every CTA of the sequence comes to the same answer: each has looked at all of its pages)
+    const bool skip = __syncthreads_or(bad) != 0;
+    if (C > 1) ptx::cluster_sync_all();  // rank 0's picks are written
+    if (skip) {
+      if (tid == 0) set_status(status, CAOTE_ERR_BAD_PAGE);
+      k = 0;
+    } else {
+      const int* E = k <= sel::kMaxSharedPicks ? s_picks : out;
+      if (rank > 0 && k <= sel::kMaxSharedPicks) {
+        for (int i = tid; i < k; i += kEvictThreads) s_picks[i] = out[i];
+        __syncthreads();
+      }
+      // The i-th survivor among slots [left, n) moves into the i-th hole below `left`. First where from and where to, a thread per
+      // slot; then half a warp per row of up to 256 bytes, several rows on their way at once.
+      const int holes = sel::lower_bound(E, k, left);
+      const int glanes = row_bytes <= 256 ? 16 : 32, gl = lane & (glanes - 1);
+      const int group = warp * (32 / glanes) + lane / glanes, groups = (kEvictThreads / 32) * (32 / glanes);
+      const int share = (k + C - 1) / C, from = rank * share, to = min(k, from + share);
+      for (int t0 = from; t0 < to; t0 += kMoves) {
+        if (t0 > from) __syncthreads();
+        const int moves = min(kMoves, to - t0);
+        for (int t = tid; t < moves; t += kEvictThreads) {
+          const int src = left + t0 + t, lb = holes + sel::lower_bound(E + holes, k - holes, src);
+          int2 mv = make_int2(-1, -1);
+          if (!(lb < k && E[lb] == src)) mv = make_int2((int)row(src), (int)row(E[t0 + t - (lb - holes)]));
+          s_moves[t] = mv;
+        }
+        __syncthreads();
+        constexpr int kAtOnce = 4;
+        for (int g0 = group; g0 < moves; g0 += kAtOnce * groups) {
+          uint4 kr[kAtOnce], vr[kAtOnce];
+          int2 mv[kAtOnce];
+#pragma unroll
+          for (int e = 0; e < kAtOnce; ++e) {
+            const int g = g0 + e * groups;
+            mv[e] = g < moves ? s_moves[g] : make_int2(-1, -1);
+            if (mv[e].x >= 0 && gl * 16 < row_bytes) {
+              kr[e] = *reinterpret_cast<const uint4*>(pool.K + (size_t)mv[e].x * row_bytes + gl * 16);
+              vr[e] = *reinterpret_cast<const uint4*>(pool.V + (size_t)mv[e].x * row_bytes + gl * 16);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < kAtOnce; ++e) {
+            if (mv[e].x < 0) continue;
+            if (gl * 16 < row_bytes) {
+              *reinterpret_cast<uint4*>(pool.K + (size_t)mv[e].y * row_bytes + gl * 16) = kr[e];
+              *reinterpret_cast<uint4*>(pool.V + (size_t)mv[e].y * row_bytes + gl * 16) = vr[e];
+            }
+            if (gl == 0) {
+              pool.mass[mv[e].y] = pool.mass[mv[e].x];
+              pool.pos[mv[e].y] = pool.pos[mv[e].x];
+            }
+          }
+        }
       }
     }
   }
-  sel::finish_lengths(dm.B, len, n_evict, ticket);
+  if (h == 0 && rank == 0 && tid == 0) n_evict[b] = k;
+  if (by_sequence) {
+    ptx::cluster_sync_all();  // every pair has read the length
+    if (h == 0 && tid == 0) len[b] = n - k;
+  } else {
+    sel::finish_lengths(dm.B, len, n_evict, ticket);
+  }
 }
 
 }  // namespace paged

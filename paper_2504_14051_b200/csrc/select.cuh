@@ -25,8 +25,10 @@ __device__ __forceinline__ unsigned long long make_key(float score, int pos) { r
 // against one another by (score bits, position), a thread per token. Mostly that is one pass. Where more tokens than that
 // have the score at the threshold, the search goes on over their positions. (Up to eight passes of 8 bits over 64-bit keys:
 // 8 units, n 4224, k 128: 17.5 -> 15.2 us between events; n 16 896, k 512, scores read again in every pass: 53 -> 36 us.)
-// score(j), position(j): a token's score bits and its position, of whatever the cache looks like.
-template <int kC, typename Score, typename Position>
+// score(first, n, v): the score bits of tokens first + i * kSelThreads < n, of whatever the cache looks like; position(j): a token's
+// position. kLast: tokens with all bits set are
+// left out of the search where there are k others (many of them would share one counter, and widen the range of bits).
+template <int kC, bool kLast = false, typename Score, typename Position>
 __device__ __forceinline__ void select_cached(int n, int k, Score score, Position position, int* out, int* picks) {
   constexpr int kW = kSelThreads / 32;
   constexpr unsigned kRank = 128u;
@@ -37,18 +39,31 @@ __device__ __forceinline__ void select_cached(int n, int k, Score score, Positio
   __shared__ int s_cnt[kC * kW];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   unsigned v[kC], live = 0u;  // score bits, and which of them are there; later the positions of the tokens at the threshold
+  score(tid, n, v);
 #pragma unroll
-  for (int i = 0; i < kC; ++i) {
-    const int j = tid + i * kSelThreads;
-    v[i] = j < n ? score(j) : 0u;
-    live |= (j < n ? 1u : 0u) << i;
-  }
+  for (int i = 0; i < kC; ++i) live |= (tid + i * kSelThreads < n ? 1u : 0u) << i;
   hist[tid] = 0u;
   hist[tid + kSelThreads] = 0u;
   if (tid == 0) s_list = 0u;
+  unsigned left = (unsigned)n;
+  if constexpr (kLast) {
+    unsigned others = live;
+#pragma unroll
+    for (int i = 0; i < kC; ++i)
+      if (v[i] == 0xffffffffu) others &= ~(1u << i);
+    const unsigned mine = __reduce_add_sync(0xffffffffu, (unsigned)__popc(others));
+    if (lane == 0) s_tot[warp] = mine;
+    __syncthreads();
+    const unsigned all = __reduce_add_sync(0xffffffffu, s_tot[lane]);
+    if (all >= (unsigned)k) {
+      live = others;
+      left = all;
+    }
+    __syncthreads();  // (s_tot is written again below)
+  }
   // thr: the threshold so far as it is known (prefix, then zeros); bits [0, top) of it are still to be decided;
   // want: how many to take of the `left` tokens with this prefix
-  unsigned thr, want = (unsigned)k, left = (unsigned)n, taken = 0u;
+  unsigned thr, want = (unsigned)k, taken = 0u;
   int top;  // 0 .. 32 (a caller's own scores may have any bits)
   auto above = [](unsigned x, int t) { return __funnelshift_rc(x, 0u, t); };  // x >> t, also for t = 32
   auto alive = [&](int i) { return (live >> i & 1u) != 0u; };

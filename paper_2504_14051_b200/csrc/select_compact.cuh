@@ -71,9 +71,16 @@ __device__ __forceinline__ int select_unit(int unit, int Hkv, int cap, const flo
 
   int* picks = (e_smem && k <= kMaxSharedPicks) ? e_smem : nullptr;
   auto score = [=](int j) { return __float_as_uint(sc[j]); };
+  auto batch = [=](int first, int count, auto& v) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(v) / sizeof(v[0])); ++i) {
+      const int j = first + i * kSelThreads;
+      v[i] = j < count ? score(j) : 0u;
+    }
+  };
   auto position = [=](int j) { return (unsigned)(ps ? ps[j] : j); };
-  if (n <= 8 * kSelThreads) select_cached<8>(n, k, score, position, out, picks);
-  else if (n <= kMaxCached * kSelThreads) select_cached<kMaxCached>(n, k, score, position, out, picks);
+  if (n <= 8 * kSelThreads) select_cached<8>(n, k, batch, position, out, picks);
+  else if (n <= kMaxCached * kSelThreads) select_cached<kMaxCached>(n, k, batch, position, out, picks);
   else select_long(n, k, score, position, out, picks);
   return k;
 }
