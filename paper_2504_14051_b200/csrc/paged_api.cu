@@ -80,7 +80,7 @@ static long long split_rows(const PDims& dm, int dtype) {
 // (4 bytes per slot and row); without, up to 32.
 constexpr int kFewRowsMass = 16, kFewRows = 32;
 static bool few_rows(const PDims& dm, int dtype, bool mass) {
-  const long long tiles = (((long long)dm.max_pages << dm.page_shift) + few::kTok - 1) / few::kTok * dm.B * dm.Hkv;
+  const long long tiles = ((long long)dm.max_pages << dm.page_shift) / 16 * dm.B * dm.Hkv;  // (at most)
   return dtype == CAOTE_BF16 && dm.max_pages > 0 && dm.scale > 0.f && (long long)dm.max_new * dm.G <= (mass ? kFewRowsMass : kFewRows) &&
          tiles < (1LL << 31) && dm.B * dm.Hkv <= 65535;
 }
@@ -104,9 +104,10 @@ static size_t carve(const PDims& dm, int dtype, char* base, Scratch* out) {
     const long long r = (long long)dm.max_new * dm.G;
     const size_t rows = r > kFewRows ? kFewRows : (size_t)(r + 7) / 8 * 8, pairs = (size_t)dm.B * dm.Hkv;
     s.rec.slots = dm.max_pages << dm.page_shift;
-    s.rec.plan = reinterpret_cast<int*>(take((size_t)dm.B + 2));
-    s.rec.stat = take((pairs + few_workers()) * rows);
-    s.rec.o = take((pairs + few_workers()) * rows * dm.D);
+    s.rec.plan = reinterpret_cast<int*>(take((size_t)dm.B + 1));
+    const size_t records = pairs + few_workers();
+    s.rec.stat = take(records * rows);
+    s.rec.o = take(records * rows * dm.D);
     s.rec.logits = take(pairs * s.rec.slots * (rows > kFewRowsMass ? kFewRowsMass : rows));
     if (off > most) most = off;
   }
@@ -240,16 +241,17 @@ static int attend_few(const PDims& dm, const Seqs& sq, const void* q, const void
   if (!mass) sc.rec.logits = nullptr;
   int* status = reinterpret_cast<int*>(ws);
   CUtensorMap tmK, tmV;
-  int rc = encode_keys(dm, K, true, few::kTok, &tmK);
-  if (!rc) rc = encode_keys(dm, V, true, few::kTok, &tmV);
+  int rc = encode_keys(dm, K, true, 16, &tmK);
+  if (!rc) rc = encode_keys(dm, V, true, 16, &tmV);
   if (!rc) rc = allow_smem(few::decode_kernel<D, NT>, few::decode_smem<D>());
   if (rc) return rc;
   CAOTE_LAUNCH("paged_decode_kernel", st,
                launch_pdl(few::decode_kernel<D, NT>, dim3(g_sm_count), dim3(few::kThreads), few::decode_smem<D>(), st, tmK, tmV, dm, sq,
                           (const __nv_bfloat16*)q, sc.rec, status));
-  const int chunks = mass ? (sc.rec.slots + few::kChunk - 1) / few::kChunk : 1;
+  const int pieces = mass ? (sc.rec.slots + few::kChunk - 1) / few::kChunk : 0;
   CAOTE_LAUNCH("paged_finish_kernel", st,
-               launch_pdl(few::finish_kernel<D, NT>, dim3(chunks, dm.B * dm.Hkv), dim3(256), 0, st, dm, sq, sc.rec, (__nv_bfloat16*)o, lse, mass,
+               launch_pdl(few::finish_kernel<D, NT>, dim3(1 + pieces, dm.B * dm.Hkv), dim3(few::kFinishThreads), 0, st, dm, sq, sc.rec, few_workers(),
+                          (__nv_bfloat16*)o, lse, mass,
                           status));
   return CAOTE_OK;
 }
