@@ -18,7 +18,7 @@ static bool params_ok(const caote_paged_params_t* p, bool pages) {
   if (p->batch < 1 || p->n_kv_heads < 1 || p->n_q_heads < 1 || p->total_new < 1 || p->max_new < 1) return false;
   if (p->n_q_heads % p->n_kv_heads != 0 || p->n_q_heads / p->n_kv_heads > 16 || p->n_kv_heads > 65535) return false;
   if (p->max_new > p->total_new || p->flags != 0 || !(p->scale == p->scale)) return false;
-  if ((long long)p->total_new * (p->n_q_heads / p->n_kv_heads) >= (1LL << 31)) return false;
+  if ((long long)p->total_new * (p->n_q_heads / p->n_kv_heads) >= (1LL << 28)) return false;
   if (pages) {
     if (p->n_pages < 1 || p->max_pages < 1) return false;
     if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128 && p->page_size != 256) return false;
@@ -127,12 +127,18 @@ static int attend_generic(const PDims& dm, const Seqs& sq, const void* q, const 
   Scratch sc;
   carve(dm, std::is_same<T, float>::value ? CAOTE_F32 : CAOTE_BF16, ws + kHeaderBytes, &sc);
   int* status = reinterpret_cast<int*>(ws);
-  auto run = [&](auto rpt) -> int {
-    constexpr int RPT = decltype(rpt)::value, kRows = generic::kRows<RPT>;
-    const size_t smem = generic::smem_bytes<D, RPT>();
-    const long long blocks = ((long long)dm.T * dm.G + dm.B * (kRows - 1LL)) / kRows;  // (no way to lie makes more)
+  const long long cap = (long long)dm.max_pages << dm.page_shift;
+  auto row_blocks = [&](int rows) { return ((long long)dm.T * dm.G + dm.B * (rows - 1LL)) / rows; };  // (no way to lie makes more)
+  auto key_blocks = [&](int keys) { return kPaged ? dm.B * ((cap + keys - 1) / keys) : ((long long)dm.T + dm.B * (keys - 1LL)) / keys; };
+  if (key_blocks(16) > 0x7fffffffLL) return CAOTE_ERR_UNSUPPORTED;
+  // Sixteen rows per CTA where sequences have no more, and 32 where 64 leave SMs idle (prompts of 243, 363 and 95 tokens, 4/2 heads,
+  // 64 channels: 55 us with 64, 29 with 16, 26 with 32).
+  auto attention = [&](auto rpt) -> int {
+    constexpr int RPT = decltype(rpt)::value;
+    const size_t smem = generic::attend_smem<D, RPT>();
+    const long long blocks = row_blocks(generic::kRows<RPT>);
     long long splits = 2LL * g_sm_count / (blocks * dm.Hkv);
-    const long long tiles = kPaged ? (((long long)dm.max_pages << dm.page_shift) + generic::kKeys - 1) / generic::kKeys : 0;
+    const long long tiles = kPaged ? (cap + generic::kKeys - 1) / generic::kKeys : 0;
     if (splits > tiles / generic::kLeastTiles) splits = tiles / generic::kLeastTiles;
     if (splits > kMostSplits) splits = kMostSplits;
     if (splits < 1) splits = 1;
@@ -146,18 +152,25 @@ static int attend_generic(const PDims& dm, const Seqs& sq, const void* q, const 
                    launch_pdl(generic::combine_kernel<T, D>, dim3((unsigned)(((long long)dm.T * dm.Hq + 7) / 8)), dim3(256), 0, st, dm, sq,
                               (int)splits, generic::kKeys, generic::kLeastTiles, (const float*)sc.opart, (const float*)sc.lpart, (T*)o, lse,
                               sc.lse2));
-    if (mass) {
-      const long long kb = kPaged ? (long long)dm.B * tiles : (long long)dm.T / generic::kKeys + dm.B;
-      if (kb > 0x7fffffffLL) return CAOTE_ERR_UNSUPPORTED;
-      rc = allow_smem(generic::mass_kernel<T, D, RPT, kPaged>, smem);
-      if (rc) return rc;
-      CAOTE_LAUNCH("paged_mass_generic", st,
-                   launch_pdl(generic::mass_kernel<T, D, RPT, kPaged>, dim3((unsigned)kb, dm.Hkv), dim3(generic::kThreads), smem, st, dm, sq,
-                              (const T*)q, (const T*)K, (const float*)sc.lse2, mass, status));
-    }
     return CAOTE_OK;
   };
-  return generic::rows_per_thread(dm.max_new * dm.G) == 1 ? run(std::integral_constant<int, 1>{}) : run(std::integral_constant<int, 4>{});
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 4> four;
+  const std::integral_constant<int, 2> two;
+  int rc = dm.max_new * dm.G <= 24 ? attention(one) : row_blocks(64) * dm.Hkv < 2 * g_sm_count ? attention(two) : attention(four);
+  if (rc || !mass) return rc;
+  auto weights = [&](auto rpt, auto kpt) -> int {
+    constexpr int RPT = decltype(rpt)::value, KPT = decltype(kpt)::value;
+    const size_t smem = generic::mass_smem<D, RPT, KPT>();
+    int rc = allow_smem(generic::mass_kernel<T, D, RPT, KPT, kPaged>, smem);
+    if (rc) return rc;
+    CAOTE_LAUNCH("paged_mass_generic", st,
+                 launch_pdl(generic::mass_kernel<T, D, RPT, KPT, kPaged>, dim3((unsigned)key_blocks(16 * KPT), dm.Hkv), dim3(generic::kThreads), smem,
+                            st, dm, sq, (const T*)q, (const T*)K, (const float*)sc.lse2, mass, status));
+    return CAOTE_OK;
+  };
+  if (dm.max_new * dm.G <= 24) return weights(one, four);
+  return key_blocks(64) * dm.Hkv < 2 * g_sm_count ? weights(four, one) : weights(four, four);
 }
 
 // ---- the tensor-core path -------------------------------------------------------------------------------

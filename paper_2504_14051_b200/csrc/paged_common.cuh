@@ -21,6 +21,14 @@ struct PDims {
   long long q_stride, kv_stride;  // elements from one packed token to the next
 };
 
+// Row numbers of a pair divided by G, by a multiplication: exact below 2^28, as many as a call may have.
+struct GroupDiv {
+  unsigned magic;
+  int g;
+  __device__ explicit GroupDiv(int g_) : magic(0xffffffffu / (unsigned)g_ + 1u), g(g_) {}
+  __device__ __forceinline__ int operator()(int r) const { return g == 1 ? r : (int)__umulhi((unsigned)r, magic); }
+};
+
 // Where the sequences begin, how long they are.
 struct Seqs {
   const int* cu;

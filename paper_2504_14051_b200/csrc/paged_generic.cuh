@@ -3,9 +3,9 @@
 //
 //   attend_kernel    kRows query rows of a (sequence, KV head) pair against its keys (or one of their splits), 64 keys at a
 //                    time: logits, running maximum and sum per row, output. A thread has RPT rows x 4 keys of the logits
-//                    and RPT rows x D / 16 channels of the output.
+//                    and RPT rows x D / 16 channels of the output. Copies of K and V take turns with the arithmetic.
 //   combine_kernel   o = sum_s o_s 2^(lse_s - lse) over the splits of a row.
-//   mass_kernel      64 keys against all rows that see them: the logits again, 2^(s - lse) summed over the rows. Every
+//   mass_kernel      16 KPT keys against all rows that see them: the logits again, 2^(s - lse) summed over the rows. Every
 //                    key's sum is formed by one CTA in a fixed order.
 //
 // What bounds them: shared-memory reads, 8 of 16 bytes for 64 multiply-adds in the logits (RPT 4).
@@ -24,61 +24,66 @@ template <int D>
 constexpr int kPitch = D + 4;  // pitch of q, K and V rows: 16 bytes further per row, so that 16 rows read without conflicts
 template <int RPT>
 constexpr int kRows = 16 * RPT;
-inline int rows_per_thread(int rows) { return rows > 24 ? 4 : 1; }
-
 template <int D, int RPT>
-constexpr size_t smem_bytes() { return sizeof(float) * (size_t)((kRows<RPT> + kKeys) * kPitch<D> + kRows<RPT> * kP) + 64; }
+constexpr size_t attend_smem() { return sizeof(float) * (size_t)((kRows<RPT> + 2 * kKeys) * kPitch<D> + kRows<RPT> * kP) + 64; }
+template <int D, int RPT, int KPT>
+constexpr size_t mass_smem() { return sizeof(float) * (size_t)((2 * kRows<RPT> + 16 * KPT) * kPitch<D> + 16 * kP) + 64; }
 
-// Rows of q into shared memory, padded with zeros: row r0 + i of the pair.
+// Four elements into shared memory as floats: fp32 by an asynchronous copy of the thread's own, bf16 through registers.
+__device__ __forceinline__ void put4(float* dst, const float* src, bool there) { ptx::cp_async16(dst, src, there); }
+__device__ __forceinline__ void put4(float* dst, const __nv_bfloat16* src, bool there) {
+  *reinterpret_cast<float4*>(dst) = there ? load4(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+// Rows of q into shared memory, padded with zeros: row r0 + i of the pair. One group of copies.
 template <typename T, int D, int RPT>
-__device__ __forceinline__ void load_rows(const PDims& dm, const T* __restrict__ q, const Seq& s, int h, int r0, float* Qs) {
+__device__ __forceinline__ void load_rows(const PDims& dm, const GroupDiv& by_g, const T* __restrict__ q, const Seq& s, int h, int r0, float* Qs) {
   const int R = s.m * dm.G;
   for (int i = threadIdx.x; i < kRows<RPT> * (D / 4); i += kThreads) {
     const int row = i / (D / 4), c = i % (D / 4), r = r0 + row;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < R) v = load4(q + (size_t)(s.t0 + r / dm.G) * dm.q_stride + (size_t)(h * dm.G + r % dm.G) * D + 4 * c);
-    *reinterpret_cast<float4*>(Qs + row * kPitch<D> + 4 * c) = v;
+    const bool there = r < R;
+    const int t = by_g(r);
+    put4(Qs + row * kPitch<D> + 4 * c, there ? q + (size_t)(s.t0 + t) * dm.q_stride + (size_t)(h * dm.G + r - t * dm.G) * D + 4 * c : q, there);
   }
+  ptx::cp_async_commit();
 }
-// 64 rows of K or V from slot j0 on; rows behind the length are zeros (whatever lies there does not reach a product).
-template <typename T, int D, bool kPaged>
+// 16 KPT rows of K or V from slot j0 on; rows behind the length are zeros (whatever lies there does not reach a product). One group.
+template <typename T, int D, int KPT, bool kPaged>
 __device__ __forceinline__ void load_keys(const PDims& dm, const Seqs& sq, const T* __restrict__ X, const Seq& s, int b, int h, int j0,
                                           float* Xs, int* status) {
-  for (int i = threadIdx.x; i < kKeys * (D / 4); i += kThreads) {
+  for (int i = threadIdx.x; i < 16 * KPT * (D / 4); i += kThreads) {
     const int row = i / (D / 4), c = i % (D / 4), j = j0 + row;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (j < s.n) {
-      const size_t at = kPaged ? pool_row(dm, sq, b, h, j, status) * D : (size_t)(s.t0 + j) * dm.kv_stride + (size_t)h * D;
-      v = load4(X + at + 4 * c);
-    }
-    *reinterpret_cast<float4*>(Xs + row * kPitch<D> + 4 * c) = v;
+    const bool there = j < s.n;
+    size_t at = 0;
+    if (there) at = (kPaged ? pool_row(dm, sq, b, h, j, status) * D : (size_t)(s.t0 + j) * dm.kv_stride + (size_t)h * D) + 4 * c;
+    put4(Xs + row * kPitch<D> + 4 * c, X + at, there);
   }
+  ptx::cp_async_commit();
 }
 // Logits in the log2 domain of rows ty * RPT + r and keys tx + 16 c.
-template <int D, int RPT>
-__device__ __forceinline__ void logits(const float* Qs, const float* Ks, float scale2, float (&s)[RPT][4]) {
+template <int D, int RPT, int KPT>
+__device__ __forceinline__ void logits(const float* Qs, const float* Ks, float scale2, float (&s)[RPT][KPT]) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
   for (int r = 0; r < RPT; ++r)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) s[r][c] = 0.f;
+    for (int c = 0; c < KPT; ++c) s[r][c] = 0.f;
 #pragma unroll 4
   for (int k = 0; k < D; k += 4) {
-    float4 kv[4];
+    float4 kv[KPT];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) kv[c] = *reinterpret_cast<const float4*>(Ks + (tx + 16 * c) * kPitch<D> + k);
+    for (int c = 0; c < KPT; ++c) kv[c] = *reinterpret_cast<const float4*>(Ks + (tx + 16 * c) * kPitch<D> + k);
 #pragma unroll
     for (int r = 0; r < RPT; ++r) {
       const float4 qv = *reinterpret_cast<const float4*>(Qs + (ty * RPT + r) * kPitch<D> + k);
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < KPT; ++c)
         s[r][c] = fmaf(qv.w, kv[c].w, fmaf(qv.z, kv[c].z, fmaf(qv.y, kv[c].y, fmaf(qv.x, kv[c].x, s[r][c]))));
     }
   }
 #pragma unroll
   for (int r = 0; r < RPT; ++r)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) s[r][c] *= scale2;
+    for (int c = 0; c < KPT; ++c) s[r][c] *= scale2;
 }
 
 // grid = (row blocks of all sequences, Hkv, splits).
@@ -90,8 +95,9 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
   ptx::pdl_trigger();
   extern __shared__ __align__(16) float smf[];
   float* Qs = smf;
-  float* Xs = Qs + kRows<RPT> * kPitch<D>;
-  float* Ps = Xs + kKeys * kPitch<D>;
+  float* Ks = Qs + kRows<RPT> * kPitch<D>;
+  float* Vs = Ks + kKeys * kPitch<D>;
+  float* Ps = Vs + kKeys * kPitch<D>;
   int* where = reinterpret_cast<int*>(Ps + kRows<RPT> * kP);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = blockIdx.y, split = blockIdx.z;
   if (tid < 32) {
@@ -107,6 +113,7 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
   const int b = where[0], r0 = where[1] * kRows<RPT>;
   if (b < 0) return;
   const Seq s = sequence(dm, sq, b);
+  const GroupDiv by_g(dm.G);
   const int R = s.m * dm.G, first = s.n - s.m;  // row r sees slots up to first + r / G
   const int last_row = min(r0 + kRows<RPT>, R) - 1;
   int per, count;
@@ -114,14 +121,19 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
   if (split >= count) return;
   const int tiles = (first + last_row / dm.G) / kKeys + 1;  // that any row of the block sees
   const int kt0 = split * per, kt1 = min(kt0 + per, tiles);
-  load_rows<T, D, RPT>(dm, q, s, h, r0, Qs);
+  // K of the next tile is on its way while V of this one is used, and the other way round
+  if (kt0 < kt1) {
+    load_rows<T, D, RPT>(dm, by_g, q, s, h, r0, Qs);
+    load_keys<T, D, 4, kPaged>(dm, sq, K, s, b, h, kt0 * kKeys, Ks, status);
+    load_keys<T, D, 4, kPaged>(dm, sq, V, s, b, h, kt0 * kKeys, Vs, status);
+  }
   const float scale2 = dm.scale * kLog2e;
   float top[RPT], l[RPT], acc[RPT][D / 16];
   int sees[RPT];
 #pragma unroll
   for (int r = 0; r < RPT; ++r) {
     const int row = r0 + ty * RPT + r;
-    sees[r] = row < R ? first + row / dm.G : -1;
+    sees[r] = row < R ? first + by_g(row) : -1;
     top[r] = -INFINITY;
     l[r] = 0.f;
 #pragma unroll
@@ -129,11 +141,10 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
   }
   for (int kt = kt0; kt < kt1; ++kt) {
     const int j0 = kt * kKeys;
-    __syncthreads();
-    load_keys<T, D, kPaged>(dm, sq, K, s, b, h, j0, Xs, status);
+    ptx::cp_async_wait<1>();
     __syncthreads();
     float x[RPT][4];
-    logits<D, RPT>(Qs, Xs, scale2, x);
+    logits<D, RPT, 4>(Qs, Ks, scale2, x);
 #pragma unroll
     for (int r = 0; r < RPT; ++r) {
       float mx = -INFINITY;
@@ -161,7 +172,9 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
       for (int c = 0; c < D / 16; ++c) acc[r][c] *= keep;
     }
     __syncthreads();
-    load_keys<T, D, kPaged>(dm, sq, V, s, b, h, j0, Xs, status);
+    if (kt + 1 < kt1) load_keys<T, D, 4, kPaged>(dm, sq, K, s, b, h, j0 + kKeys, Ks, status);
+    else ptx::cp_async_commit();  // (an empty group in its place)
+    ptx::cp_async_wait<1>();
     __syncthreads();
 #pragma unroll 2
     for (int j = 0; j < kKeys; j += 4) {
@@ -172,7 +185,7 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
       for (int e = 0; e < 4; ++e) {
         float4 vv[D / 64];
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) vv[c] = *reinterpret_cast<const float4*>(Xs + (j + e) * kPitch<D> + 64 * c + 4 * tx);
+        for (int c = 0; c < D / 64; ++c) vv[c] = *reinterpret_cast<const float4*>(Vs + (j + e) * kPitch<D> + 64 * c + 4 * tx);
 #pragma unroll
         for (int r = 0; r < RPT; ++r) {
           const float p = e == 0 ? pv[r].x : (e == 1 ? pv[r].y : (e == 2 ? pv[r].z : pv[r].w));
@@ -186,6 +199,9 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
         }
       }
     }
+    __syncthreads();
+    if (kt + 1 < kt1) load_keys<T, D, 4, kPaged>(dm, sq, V, s, b, h, j0 + kKeys, Vs, status);
+    else ptx::cp_async_commit();
   }
 #pragma unroll
   for (int r = 0; r < RPT; ++r) {
@@ -257,65 +273,75 @@ combine_kernel(PDims dm, Seqs sq, int splits, int keys_per_tile, int least_tiles
   }
 }
 
-// grid = (key blocks of all sequences, Hkv). Prompts: mass[t, h] = sum; pages: mass[page, h, row] += sum.
-template <typename T, int D, int RPT, bool kPaged>
+// grid = (blocks of 16 KPT keys of all sequences, Hkv). Prompts: mass[t, h] = sum; pages: mass[page, h, row] += sum.
+template <typename T, int D, int RPT, int KPT, bool kPaged>
 __global__ void __launch_bounds__(kThreads)
 mass_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ K, const float* __restrict__ lse2,
             float* __restrict__ mass, int* status) {
+  constexpr int kMine = 16 * KPT;
   ptx::pdl_wait();
   ptx::pdl_trigger();
   extern __shared__ __align__(16) float smf[];
-  float* Qs = smf;
-  float* Xs = Qs + kRows<RPT> * kPitch<D>;
-  float* Ps = Xs + kKeys * kPitch<D>;  // [16][kP] in the end; before, the rows' statistics
-  int* where = reinterpret_cast<int*>(Ps + kRows<RPT> * kP);
+  float* Qs = smf;  // [2] blocks of rows
+  float* Ks = Qs + 2 * kRows<RPT> * kPitch<D>;
+  float* sums = Ks + kMine * kPitch<D>;  // [16][kP]
+  int* where = reinterpret_cast<int*>(sums + 16 * kP);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, h = blockIdx.y;
   if (tid < 32) {
     auto what = [&](const Seq& x) { return x.m > 0 ? x.n : 0; };
     Place p;
-    Scan c = scan(dm, sq, 0, kKeys, what, nullptr);
-    const bool there = find_block(dm, sq, kKeys, blockIdx.x, what, c, p);
+    Scan c = scan(dm, sq, 0, kMine, what, nullptr);
+    const bool there = find_block(dm, sq, kMine, blockIdx.x, what, c, p);
     if (tid == 0) { where[0] = there ? p.b : -1; where[1] = p.block; }
   }
   __syncthreads();
-  const int b = where[0], j0 = where[1] * kKeys;
+  const int b = where[0], j0 = where[1] * kMine;
   if (b < 0) return;
   const Seq s = sequence(dm, sq, b);
+  const GroupDiv by_g(dm.G);
   const int R = s.m * dm.G, first = s.n - s.m;
-  load_keys<T, D, kPaged>(dm, sq, K, s, b, h, j0, Xs, status);
   const float scale2 = dm.scale * kLog2e;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  float sum[KPT];
+#pragma unroll
+  for (int c = 0; c < KPT; ++c) sum[c] = 0.f;
   // the first row that sees any of these keys
-  int r_begin = max(0, j0 - first) * dm.G;
-  r_begin -= r_begin % kRows<RPT>;
-  for (int r0 = r_begin; r0 < R; r0 += kRows<RPT>) {
+  int r0 = max(0, j0 - first) * dm.G;
+  r0 -= r0 % kRows<RPT>;
+  load_keys<T, D, KPT, kPaged>(dm, sq, K, s, b, h, j0, Ks, status);
+  load_rows<T, D, RPT>(dm, by_g, q, s, h, r0, Qs);
+  const float* stats = lse2 + stat_at(dm, s, h, 0);
+  for (int buf = 0; r0 < R; r0 += kRows<RPT>, buf ^= 1) {
+    float stat[RPT];
+#pragma unroll
+    for (int r = 0; r < RPT; ++r) stat[r] = r0 + ty * RPT + r < R ? stats[r0 + ty * RPT + r] : 0.f;
+    // the next block of rows goes where the one before this lay (the barrier at the end)
+    if (r0 + kRows<RPT> < R) load_rows<T, D, RPT>(dm, by_g, q, s, h, r0 + kRows<RPT>, Qs + (buf ^ 1) * kRows<RPT> * kPitch<D>);
+    else ptx::cp_async_commit();
+    ptx::cp_async_wait<1>();
     __syncthreads();
-    load_rows<T, D, RPT>(dm, q, s, h, r0, Qs);
-    if (tid < kRows<RPT>) {
-      const int r = r0 + tid;
-      Ps[tid] = r < R ? lse2[stat_at(dm, s, h, r)] : 0.f;
-    }
-    __syncthreads();
-    float x[RPT][4];
-    logits<D, RPT>(Qs, Xs, scale2, x);
+    float x[RPT][KPT], part[KPT];
+    logits<D, RPT, KPT>(Qs + buf * kRows<RPT> * kPitch<D>, Ks, scale2, x);
+#pragma unroll
+    for (int c = 0; c < KPT; ++c) part[c] = 0.f;
 #pragma unroll
     for (int r = 0; r < RPT; ++r) {
       const int row = r0 + ty * RPT + r;
-      const int sees = row < R ? first + row / dm.G : -1;
-      const float stat = Ps[ty * RPT + r];
+      const int sees = row < R ? first + by_g(row) : -1;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (j0 + tx + 16 * c <= sees) sum[c] += ptx::fast_exp2(x[r][c] - stat);
+      for (int c = 0; c < KPT; ++c)
+        if (j0 + tx + 16 * c <= sees) part[c] += ptx::fast_exp2(x[r][c] - stat[r]);
     }
-  }
-  __syncthreads();
 #pragma unroll
-  for (int c = 0; c < 4; ++c) Xs[ty * kP + tx + 16 * c] = sum[c];
+    for (int c = 0; c < KPT; ++c) sum[c] += part[c];
+    __syncthreads();
+  }
+#pragma unroll
+  for (int c = 0; c < KPT; ++c) sums[ty * kP + tx + 16 * c] = sum[c];
   __syncthreads();
-  if (tid < kKeys && j0 + tid < s.n) {
+  if (tid < kMine && j0 + tid < s.n) {
     float v = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v += Xs[i * kP + tid];
+    for (int i = 0; i < 16; ++i) v += sums[i * kP + tid];
     if (kPaged) mass[pool_row(dm, sq, b, h, j0 + tid, status)] += v;
     else mass[(size_t)(s.t0 + j0 + tid) * dm.Hkv + h] = v;
   }

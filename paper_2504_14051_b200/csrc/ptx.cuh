@@ -65,6 +65,15 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
       : "memory");
 }
+// 16 bytes global -> shared by the thread itself, asynchronously, zeros where `there` is false; groups of them closed and awaited
+// (all but the newest kLeft groups).
+__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
 // Untiled bulk copy shared -> global, alignment as above, into this thread's current bulk group; the group closed; and a wait until
 // the groups' sources have been read, or until they are written.
 __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
