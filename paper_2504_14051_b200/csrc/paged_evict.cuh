@@ -233,18 +233,18 @@ evict_kernel(PDims dm, Seqs sq, Pool pool, int row_bytes, int* __restrict__ len,
     if (rank == 0) {
       // (asked for where weights tie only: kept out of the way of the code that always runs)
       const Positions position{table, pos, Hkv, h, shift, n_pages};
-      // half a dozen tokens' pages, then all of their weights and positions, are on their way at a time
+      // eight or nine tokens' pages, then all of their weights and positions, are on their way at a time
       auto scores = [&](int first, int count, auto& v) {
-        constexpr int kC = (int)(sizeof(v) / sizeof(v[0])), kAtOnce = kC % 6 == 0 ? 6 : 8;
+        constexpr int kC = (int)(sizeof(v) / sizeof(v[0])), kAtOnce = kC % 9 == 0 ? 9 : 8;
         static_assert(kC % kAtOnce == 0, "");
 #pragma unroll
         for (int i0 = 0; i0 < kC; i0 += kAtOnce) {
-          size_t at[kAtOnce];
+          unsigned at[kAtOnce];  // (pools have less than 2^31 rows)
           int p[kAtOnce];
 #pragma unroll
           for (int e = 0; e < kAtOnce; ++e) {
             const int j = first + (i0 + e) * kEvictThreads;
-            at[e] = row(j < count ? j : 0);
+            at[e] = (unsigned)row(j < count ? j : 0);
           }
 #pragma unroll
           for (int e = 0; e < kAtOnce; ++e) {
