@@ -20,7 +20,7 @@
  *   page_table   [B, max_pages]     int32: slot j of sequence b lies in page page_table[b, j / page_size]. Entries behind a
  *                                   sequence's length are not read.
  *   len, n_seen, budget, n_evict [B] int32: tokens in the cache, tokens ever appended, tokens to keep, tokens evicted
- * Strides in elements, 0 = dense; q, k and v may be slices of one buffer. q, k, v, K, V, o must be 16-byte aligned, and so
+ * Outputs must not overlap inputs. Strides in elements, 0 = dense; q, k and v may be slices of one buffer. q, k, v, K, V, o must be 16-byte aligned, and so
  * must their strides in bytes; the other arrays 4-byte aligned.
  *
  * Calls that write pages (append, evict, attend with mass) need pages that belong to one sequence each. Calls that only read
@@ -49,7 +49,7 @@ typedef struct {
   int32_t page_size;  /* tokens per page: 16, 32, 64, 128 or 256. Prompts alone: 0                 */
   int32_t n_pages;    /* pages in the pool; n_pages * Hkv * page_size < 2^31. Prompts alone: 0     */
   int32_t max_pages;  /* columns of the page table. Prompts alone: 0                               */
-  int32_t total_new;  /* T >= 1                                                                    */
+  int32_t total_new;  /* T >= 1, T * G < 2^28                                                      */
   int32_t max_new;    /* most new tokens of one sequence in this call, 1 .. T                      */
   int32_t dtype;      /* caote_dtype_t of q, k, v, K, V, o                                         */
   float scale;        /* logits are scale * <q, k>                                                 */

@@ -141,10 +141,14 @@ class PagedCache:
         return C.make_paged_params(self.batch, self.Hq, self.Hkv, self.d, self.page_size, self.n_pages, self.max_pages, total,
                                    most, self.dtype, self.scale)
 
-    def _begin(self, new):
-        """Pages for the new tokens; (parameters, cu, T)."""
+    def _begin(self, new, q, k, v):
+        """Pages for the new tokens; (lengths, parameters, cu, T). Nothing has changed when it refuses."""
         new = [int(m) for m in new]
         T = sum(new)
+        for name, t, heads in (("q", q, self.Hq), ("k", k, self.Hkv), ("v", v, self.Hkv)):
+            if t.shape != (T, heads, self.d) or t.dtype is not self.dtype or t.device.type != self.device.type:
+                raise ValueError(f"PagedCache: {name} has to be {(T, heads, self.d)}, {self.dtype} on {self.device}, "
+                                 f"not {tuple(t.shape)}, {t.dtype} on {t.device}")
         if len(new) != self.batch or min(new) < 0 or not 1 <= T <= self.max_total_new:
             raise ValueError(f"PagedCache: {self.batch} sequences with 1 to {self.max_total_new} new tokens together, not {new}")
         need = [-(-(n + m) // self.page_size) for n, m in zip(self.host_lens, new)]
@@ -178,7 +182,7 @@ class PagedCache:
         """First tokens of sequences that hold none yet: attended among themselves, then put into pages."""
         if any(m and n for m, n in zip(new, self.host_lens)):
             raise ValueError("PagedCache.prompt: a sequence with a prompt already holds tokens")
-        new, p, cu, T = self._begin(new)
+        new, p, cu, T = self._begin(new, q, k, v)
         o, mass = self.o[:T], self.mass_new[:T]
         C.caote_prompt_attend(p, q, k, v, cu, o, self.lse[:T], mass, self.workspace)
         C.caote_paged_append(p, self.K, self.V, self.mass, self.pos, self.page_table, self.lens, self.n_seen, k, v, mass, cu,
@@ -188,7 +192,7 @@ class PagedCache:
 
     def step(self, q, k, v, new):
         """More tokens of some sequences: into the pages, then attended over everything there."""
-        new, p, cu, T = self._begin(new)
+        new, p, cu, T = self._begin(new, q, k, v)
         C.caote_paged_append(p, self.K, self.V, self.mass, self.pos, self.page_table, self.lens, self.n_seen, k, v, None, cu,
                              self.workspace)
         o = self.o[:T]

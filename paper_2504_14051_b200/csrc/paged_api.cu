@@ -62,10 +62,12 @@ struct Scratch {
   float* lse2;   // [Hkv, T, G] log2-domain log-sum-exp of every row
   float* lpart;  // [splits, T, Hq] and
   float* opart;  // [splits, T, Hq, D]: what the splits of the keys contribute
+  float* mass_part;  // prompts: [kMostChunks, T, Hkv] the weights received from the chunks of a prompt's rows
   tcore::SplitNote* notes;  // [1 + SMs] which items' keys were split
   few::Records rec;
 };
 constexpr int kMostSplits = 16;
+constexpr int kMostChunks = 8;    // of a prompt's rows, in the pass for the weights
 constexpr int kItemCounter = 12;  // word of the workspace header
 // fp32: splits are only made where the row blocks of a call leave room for two CTAs of 64 rows per SM, so splits x rows stays
 // below what these hold; a bound that grows with T and does not depend on how the rows lie. bf16: 256 rows of the last round's
@@ -97,6 +99,7 @@ static size_t carve(const PDims& dm, int dtype, char* base, Scratch* out) {
   s.lpart = take((size_t)split_rows(dm, dtype));
   s.opart = take((size_t)split_rows(dm, dtype) * dm.D);
   s.notes = reinterpret_cast<tcore::SplitNote*>(take(4 * (size_t)(1 + g_sm_count)));
+  s.mass_part = take(dtype == CAOTE_BF16 ? (size_t)kMostChunks * dm.T * dm.Hkv : 0);
   size_t most = off;
   if (dtype == CAOTE_BF16 && dm.max_pages > 0) {
     // (a workspace for more rows per sequence serves calls with fewer: sized for the most rows that come here)
@@ -225,7 +228,7 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
   const long long tiles = ((kPaged ? cap : dm.max_new) + tcore::kTile - 1) / tcore::kTile;
   const int most_splits = tiles >= 2 * tcore::kLeastTiles && (kPaged || items < 2 * g_sm_count) ? kMostSplits : 1;
   // (items of the mass kernel are numbered in 32 bits)
-  const long long key_blocks = (kPaged ? (cap + tcore::kKeys - 1) / tcore::kKeys * dm.B : (long long)dm.T / tcore::kKeys + dm.B) * dm.Hkv;
+  const long long key_blocks = (kPaged ? (cap + tcore::kKeys - 1) / tcore::kKeys * dm.B : ((long long)dm.T / tcore::kKeys + dm.B) * kMostChunks) * dm.Hkv;
   if (items > 0x7fff0000LL || key_blocks > 0x7fff0000LL) return CAOTE_ERR_UNSUPPORTED;
   CAOTE_LAUNCH("paged_attend_kernel", st,
                launch_pdl(tcore::attend_kernel<D, kPaged>, dim3((unsigned)(items + (most_splits > 1 ? g_sm_count : 0))),
@@ -235,10 +238,23 @@ static int attend_tc(const PDims& dm, const Seqs& sq, const void* q, const void*
     CAOTE_LAUNCH("paged_combine", st,
                  launch_pdl(tcore::combine_kernel<D>, dim3((unsigned)(items < g_sm_count ? items : g_sm_count - 1), 8), dim3(256), 0, st, dm, sq, (__nv_bfloat16*)o, lse, sc.lse2,
                             (const float*)sc.opart, (const float*)sc.lpart, (const tcore::SplitNote*)sc.notes));
-  if (mass)
+  if (mass) {
+    // row blocks of the longest prompt, of an SM's share if the prompts are alike, and of a chunk
+    const long long longest = (dm.max_new + tok - 1) / tok, share = (long long)dm.Hkv * dm.T / tcore::kKeys * (dm.T / dm.B / tok) / 2 / g_sm_count;
+    long long chunk = longest;
+    if (!kPaged) {
+      chunk = share / 3 > 16 ? share / 3 : 16;
+      if (chunk < (longest + kMostChunks - 1) / kMostChunks) chunk = (longest + kMostChunks - 1) / kMostChunks;
+    }
+    const int chunks = (int)((longest + chunk - 1) / chunk);
     CAOTE_LAUNCH("paged_mass_kernel", st,
                  launch_pdl(tcore::mass_kernel<D, kPaged>, dim3(g_sm_count), dim3(tcore::kMassThreads), tcore::mass_smem<D>(), st, tmQ, tmK, dm,
-                            sq, box, (const float*)sc.lse2, mass, status + kItemCounter, status));
+                            sq, box, (const float*)sc.lse2, chunks > 1 ? sc.mass_part : mass, chunks, (int)chunk, status + kItemCounter, status));
+    if (chunks > 1)
+      CAOTE_LAUNCH("paged_sum_kernel", st,
+                   launch_pdl(tcore::sum_kernel, dim3((unsigned)(((long long)dm.T * dm.Hkv + 255) / 256)), dim3(256), 0, st, dm, sq,
+                              (const float*)sc.mass_part, (int)chunk, mass));
+  }
   return CAOTE_OK;
 }
 

@@ -541,6 +541,9 @@ combine_kernel(PDims dm, Seqs sq, __nv_bfloat16* __restrict__ o, float* __restri
 // ---- the weight that every key received ------------------------------------------------------------------
 // Persistent: a CTA takes items of 256 keys from a counter, the next item's K on its way while this one's rows go by. The warps
 // that copy and issue run ahead of the key threads across items; rows, statistics and S buffers are counted through.
+// Of a prompt the first keys are seen by all rows: where that is more than a third of an SM's share, the rows are cut into chunks
+// that are items of their own and leave partial sums, which sum_kernel adds up in order (whole calls, one prompt of 6 000 tokens, 64/8
+// heads: 1 025 us in one chunk, 861 in five; of 4 000, 32/2 heads: 688 and 297).
 constexpr int kKeys = 2 * kTile;                       // keys per item
 constexpr int kKeyThreads = 2 * kKeys;                 // two threads per key: 64 rows of a row block each
 constexpr int kMassThreads = kKeyThreads + 128;        // + products, items and K, Q, statistics
@@ -573,15 +576,16 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[16], const float
 }
 
 struct Item {
-  int b, h, j0, rb0, blocks;  // b < 0: no more; rb0: the first row block (of 128 / G tokens) that sees any of the keys
+  int b, h, j0, rb0, blocks;  // b < 0: no more; row blocks (of 128 / G tokens) [rb0, rb0 + blocks) of the chunk that see any of the keys
+  int chunk;
   Seq s;
 };
 
-// grid: one CTA per SM. next_item: their number at the start (the attention pass leaves it so).
+// grid: one CTA per SM. chunks > 1 (prompts): rows in chunks of chunk_blocks blocks, mass [chunks, T, Hkv] their sums. next_item: their number at the start (the attention pass leaves it so).
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kMassThreads, 1)
 mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, PDims dm, Seqs sq, int box,
-            const float* __restrict__ lse2, float* __restrict__ mass, int* next_item, int* status) {
+            const float* __restrict__ lse2, float* __restrict__ mass, int chunks, int chunk_blocks, int* next_item, int* status) {
   constexpr int kTB = kTileBytesOf<D>, kBoxes = D / 64, kSteps = D / 16, kQS = kQStages<D>;
   if (threadIdx.x == 0) {
     ptx::prefetch_map(&tmQ);
@@ -604,7 +608,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
 
   const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
   const int tok = kTile / dm.G;
-  // the item of number `it`, its K tiles' pages (this lane's) and boxes; the warp of the items
+  // the item of number `it`, its K tiles' pages (this lane's) and boxes, false if no row of it sees a key; the warp of the items
   auto what = [](const Seq& x) { return x.m > 0 ? x.n : 0; };
   struct Next { Item x; int id[2], boxes[2]; } nx;
   Scan seqs;
@@ -613,27 +617,40 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     // last head's first keys come late: 2.84 instead of 1.4 ms, 64/8 heads, prompts of 7 428 and 8 956 tokens.)
     Place p;
     nx.id[0] = nx.id[1] = nx.boxes[0] = nx.boxes[1] = 0;
-    if (!find_block(dm, sq, kKeys, it / dm.Hkv, what, seqs, p)) {
+    const int at = it / dm.Hkv;
+    if (!find_block(dm, sq, kKeys, at / chunks, what, seqs, p)) {
       nx.x.b = -1;
-      return;
+      return true;
     }
     nx.x.b = p.b;
     nx.x.h = it % dm.Hkv;
     nx.x.s = p.s;
     nx.x.j0 = p.block * kKeys;
-    nx.x.rb0 = max(0, nx.x.j0 - (p.s.n - p.s.m)) / tok;
-    nx.x.blocks = (p.s.m + tok - 1) / tok - nx.x.rb0;
+    nx.x.chunk = at % chunks;
+    nx.x.rb0 = max(max(0, nx.x.j0 - (p.s.n - p.s.m)) / tok, nx.x.chunk * chunk_blocks);
+    nx.x.blocks = (int)min((long long)((p.s.m + tok - 1) / tok), (nx.x.chunk + 1LL) * chunk_blocks) - nx.x.rb0;
+    if (nx.x.blocks <= 0) return false;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
       if (nx.x.j0 + kk * kTile < p.s.n) {
         nx.id[kk] = page_of<kPaged>(dm, sq, p.b, p.s.n, nx.x.j0 + kk * kTile, box, status);
         nx.boxes[kk] = boxes_of<kPaged>(p.s, nx.x.j0 + kk * kTile, box);
       }
+    return true;
+  };
+  // ... the next one that has rows, from item `it` on
+  auto draw = [&]() {
+    int it = 0;
+    if ((threadIdx.x & 31) == 0) it = atomicAdd(next_item, 1);
+    return __shfl_sync(0xffffffffu, it, 0);
+  };
+  auto find_next = [&](int it) {
+    while (!find(it)) it = draw();
   };
   // the set-up's parts side by side
   if (warp == 17) {
     seqs = scan(dm, sq, 0, kKeys, what, nullptr);
-    find(blockIdx.x);
+    find_next(blockIdx.x);
   } else if (warp == 1) {
     tmem_alloc(tmem_slot, 512);
   } else if (tid == 0) {
@@ -652,11 +669,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     // =============================== items and their K (the warp) ===============================
     for (int c = 0;; ++c) {
       const int buf = c & 1;
-      if (c > 0) {
-        int it = 0;
-        if (lane == 0) it = atomicAdd(next_item, 1);
-        find(__shfl_sync(0xffffffffu, it, 0));
-      }
+      if (c > 0) find_next(draw());
       const Item& x = nx.x;
       if (c >= 2) mbar_wait_idle(&item_free[buf], ((c >> 1) - 1) & 1, status);
       if (lane == 0) {
@@ -776,7 +789,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           out = mass + pool_row(dm, sq, x.b, x.h, j, status);
           before = *out;
         } else {
-          out = mass + (size_t)(x.s.t0 + j) * dm.Hkv + x.h;
+          out = mass + ((size_t)x.chunk * dm.T + x.s.t0 + j) * dm.Hkv + x.h;
         }
       }
       for (int rb = 0; rb < x.blocks; ++rb, ++qb) {
@@ -843,6 +856,28 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// Prompts: mass = the sum over the chunks whose rows see the token. grid = ceil(T * Hkv / 256).
+__global__ void __launch_bounds__(256)
+sum_kernel(PDims dm, Seqs sq, const float* __restrict__ part, int chunk_blocks, float* __restrict__ mass) {
+  ptx::pdl_wait();
+  ptx::pdl_trigger();
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (long long)dm.T * dm.Hkv) return;
+  const int t = (int)(i / dm.Hkv), tok = kTile / dm.G;
+  int lo = 0, hi = dm.B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(sq.cu + mid) <= t) lo = mid; else hi = mid;
+  }
+  const Seq s = sequence(dm, sq, lo);
+  if (t < s.t0 || t >= s.t0 + s.m) return;
+  const int first = (t - s.t0) / kKeys * kKeys / tok / chunk_blocks, last = ((s.m + tok - 1) / tok - 1) / chunk_blocks;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int c = first; c <= last; ++c) sum += part[(size_t)c * dm.T * dm.Hkv + i];
+  mass[i] = sum;
 }
 
 }  // namespace tcore

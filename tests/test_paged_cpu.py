@@ -198,13 +198,17 @@ def test_page_bookkeeping_on_the_host(monkeypatch):
     check()
     with pytest.raises(ValueError, match="already holds"):
         c.prompt(x(1, 4), x(1, 2), x(1, 2), [1, 0, 0])
-    c._begin([100, 0, 0])  # 8 of the 12 pages
+    begin = lambda new: c._begin(new, x(sum(new), 4), x(sum(new), 2), x(sum(new), 2))  # noqa: E731
+    begin([100, 0, 0])  # 8 of the 12 pages
     with pytest.raises(ValueError, match="are free"):
-        c._begin([0, 90, 0])
+        begin([0, 90, 0])
     with pytest.raises(ValueError, match="would need"):
         c.host_lens[2] = 120
-        c._begin([0, 0, 9])
+        begin([0, 0, 9])
     c.host_lens[2] = 7
+    for bad in ((x(2, 4), x(3, 2), x(3, 2)), (x(3, 4), x(3, 4), x(3, 2)), (x(3, 4), x(3, 2), x(3, 2).double())):
+        with pytest.raises(ValueError, match="has to be"):
+            c.step(*bad, [1, 1, 1])
     check_free = len(c._free)
     with pytest.raises(ValueError):
         c.step(x(1, 4), x(1, 2), x(1, 2), [0, 0, 0])
