@@ -8,6 +8,7 @@
 //                   other's products run.
 //   mass_kernel     keys x rows. A CTA owns 256 keys of a pair and walks the rows that see them: S^T = K Q^T into TMEM, one key
 //                   per lane, so that a thread sums 2^(s - lse) over the rows of its own key without any exchange.
+//   combine_kernel  adds up what the splits of a row's keys left, sum_kernel what the chunks of a key's rows left.
 //
 // Roundings: P is rounded to bf16 once (2^-9 of each weight at most, half of that on average, of random sign); o, of which it
 // is a weighted sum, is rounded to bf16 itself, so o's error against 64 bits is sqrt(2) of what the output's type costs.
@@ -581,7 +582,8 @@ struct Item {
   Seq s;
 };
 
-// grid: one CTA per SM. chunks > 1 (prompts): rows in chunks of chunk_blocks blocks, mass [chunks, T, Hkv] their sums. next_item: their number at the start (the attention pass leaves it so).
+// grid: one CTA per SM. chunks > 1 (prompts): rows in chunks of chunk_blocks blocks, mass [chunks, T, Hkv] their sums. next_item:
+// the grid's size at the start (the attention pass leaves it so).
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kMassThreads, 1)
 mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, PDims dm, Seqs sq, int box,
