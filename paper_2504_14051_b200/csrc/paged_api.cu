@@ -353,7 +353,7 @@ int caote_paged_append(const caote_paged_params_t* p, void* K, void* V, float* m
   const int e = p->dtype == CAOTE_BF16 ? 2 : 4, row_bytes = dm.D * e;
   const long long pieces = (long long)dm.T * dm.Hkv * 2 * (row_bytes / 16);
   long long ctas = (pieces + paged::kAppendThreads - 1) / paged::kAppendThreads;
-  if (ctas > 8LL * g_sm_count) ctas = 8LL * g_sm_count;
+  if (ctas > (long long)paged::kAppendCtas * g_sm_count) ctas = (long long)paged::kAppendCtas * g_sm_count;
   CAOTE_LAUNCH("paged_append_kernel", (cudaStream_t)stream,
                launch_pdl(paged::append_kernel, dim3((unsigned)ctas), dim3(paged::kAppendThreads), 0, (cudaStream_t)stream, dm,
                           paged::Seqs{cu, len, page_table}, row_bytes, dm.kv_stride * e, (char*)K, (char*)V, mass, pos, len, n_seen,

@@ -20,9 +20,11 @@ constexpr int kEvictThreads = sel::kSelThreads;
 constexpr unsigned kSheltered = 0xffffffffu;  // as the score bits of a sheltered token: behind every other
 
 // New rows into the pages: a thread per 16 bytes of a K or V row, the pieces of a token side by side. The CTA that finishes last moves
-// the lengths on; a sequence that does not fit, or one of whose pages is none, keeps its length.
-constexpr int kAppendThreads = 256, kSharedStarts = 1024;
-__global__ void __launch_bounds__(kAppendThreads)
+// the lengths on; a sequence that does not fit, or one of whose pages is none, keeps its length. Up to as many CTAs as are resident at
+// once: more would wait for their turn (8 sequences of 512 tokens, 8 KV heads, 16.8 MB, cold: 20.5 us with five per SM, 19 with six, 20
+// with eight, whose 32 registers do not suffice; two and four tokens on their way per thread: 1 and 5 us longer).
+constexpr int kAppendThreads = 256, kAppendCtas = 6, kSharedStarts = 1024;
+__global__ void __launch_bounds__(kAppendThreads, kAppendCtas)
 append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __restrict__ K, char* __restrict__ V,
               float* __restrict__ mass, int* __restrict__ pos, int* __restrict__ len, int* __restrict__ n_seen,
               const char* __restrict__ k_new, const char* __restrict__ v_new, const float* __restrict__ mass_new, int* status,
@@ -42,13 +44,14 @@ append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __re
   const int at_once = per_token < kAppendThreads ? kAppendThreads / per_token : 1;  // tokens
   const long long cap = (long long)dm.max_pages << dm.page_shift;
   const int sub = per_token < kAppendThreads ? tid / per_token : 0, rest0 = tid - sub * per_token;
+  const int h0 = rest0 / (2 * pieces), which0 = rest0 / pieces & 1, c0 = rest0 % pieces;
   for (int t = blockIdx.x * at_once + sub; t < dm.T && sub < at_once; t += gridDim.x * at_once) {
-    auto source = [&](int rest) {
-      const int h = rest / (2 * pieces);
-      return *reinterpret_cast<const uint4*>((rest / pieces & 1 ? v_new : k_new) + (size_t)t * src_stride + (size_t)h * row_bytes + rest % pieces * 16);
+    auto source = [&](int h, int which, int c) {
+      return *reinterpret_cast<const uint4*>((which ? v_new : k_new) + (size_t)t * src_stride + (size_t)h * row_bytes + c * 16);
     };
+    int h = h0, which = which0, c = c0;
     uint4 x = make_uint4(0u, 0u, 0u, 0u);  // (on its way while the token's place is looked up)
-    if (rest0 < per_token) x = source(rest0);
+    if (rest0 < per_token) x = source(h, which, c);
     int lo = 0, hi = dm.B;  // the sequence of token t: the last one that begins at or before it
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -60,14 +63,19 @@ append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __re
     const int page = __ldg(sq.table + (size_t)lo * dm.max_pages + (j >> dm.page_shift));
     if ((unsigned)page >= (unsigned)dm.n_pages) continue;
     const size_t row0 = ((size_t)page * dm.Hkv << dm.page_shift) + (j & ((1 << dm.page_shift) - 1));  // of head 0
-    for (int rest = rest0; rest < per_token; rest += kAppendThreads) {
-      const int h = rest / (2 * pieces), which = rest / pieces & 1, c = rest % pieces;
+    for (int rest = rest0; rest < per_token;) {
       const size_t at = row0 + ((size_t)h << dm.page_shift);
-      if (rest != rest0) x = source(rest);
       *reinterpret_cast<uint4*>((which ? V : K) + at * row_bytes + c * 16) = x;
       if (which == 0 && c == 0) {
         if (mass) mass[at] = mass_new ? mass_new[(size_t)t * dm.Hkv + h] : 0.f;
         if (pos) pos[at] = seen + t - t0;
+      }
+      rest += kAppendThreads;
+      if (rest < per_token) {
+        h = rest / (2 * pieces);
+        which = rest / pieces & 1;
+        c = rest % pieces;
+        x = source(h, which, c);
       }
     }
   }
@@ -80,23 +88,32 @@ append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __re
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  for (int b = tid; b < dm.B; b += kAppendThreads) {
-    const int t0 = start(b), t1 = start(b + 1), m = t1 - t0, n = len[b];
-    if (t0 < 0 || t1 < t0 || t1 > dm.T || m > dm.max_new || n < 0) {
-      set_status(status, CAOTE_ERR_BAD_LENGTH);
-    } else if (n + (long long)m > cap) {
-      set_status(status, CAOTE_ERR_OVERFLOW);
-    } else if (m > 0) {
-      bool ok = true;
+  // (a power of two of lanes per sequence, so that one round of the CTA does where it can: they share the look at its pages)
+  int lanes = 32;
+  while (lanes > 1 && (long long)lanes * dm.B > kAppendThreads) lanes >>= 1;
+  const int lane = tid & 31, in = lane & (lanes - 1);
+  for (int b0 = 0; b0 < dm.B; b0 += kAppendThreads / lanes) {
+    const int b = b0 + tid / lanes;
+    const bool there = b < dm.B;
+    const int t0 = there ? start(b) : 0, t1 = there ? start(b + 1) : 0, m = t1 - t0, n = there ? len[b] : 0;
+    const bool sound = t0 >= 0 && t1 >= t0 && t1 <= dm.T && m <= dm.max_new && n >= 0, fits = sound && n + (long long)m <= cap;
+    bool ok = true;
+    if (fits && m > 0) {
 #pragma unroll 4
-      for (int p = n >> dm.page_shift; p <= (n + m - 1) >> dm.page_shift; ++p)
-        ok = ok && (unsigned)__ldg(sq.table + (size_t)b * dm.max_pages + p) < (unsigned)dm.n_pages;
-      if (!ok) {
-        set_status(status, CAOTE_ERR_BAD_PAGE);
-      } else {
-        len[b] = n + m;
-        if (n_seen) n_seen[b] += m;
-      }
+      for (int p = (n >> dm.page_shift) + in; p <= (n + m - 1) >> dm.page_shift; p += lanes)
+        ok &= (unsigned)__ldg(sq.table + (size_t)b * dm.max_pages + p) < (unsigned)dm.n_pages;
+    }
+    const unsigned wrong = __ballot_sync(0xffffffffu, !ok) >> (lane - in) & (unsigned)((1ull << lanes) - 1ull);
+    if (!there || in != 0) continue;
+    if (!sound) {
+      set_status(status, CAOTE_ERR_BAD_LENGTH);
+    } else if (!fits) {
+      set_status(status, CAOTE_ERR_OVERFLOW);
+    } else if (wrong != 0u) {
+      set_status(status, CAOTE_ERR_BAD_PAGE);
+    } else if (m > 0) {
+      len[b] = n + m;
+      if (n_seen) n_seen[b] += m;
     }
   }
   if (tid == 0) *ticket = 0;

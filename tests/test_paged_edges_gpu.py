@@ -287,3 +287,32 @@ def test_budget_and_counts_are_checked_before_anything_moves():
         P.caote_paged_evict(p, K.clone(), K.clone(), m.clone(), pos.clone(), pg.table.to(DEV), lens, lens.clone(),
                             torch.tensor([budget], dtype=torch.int32, device=DEV), 0, 0, torch.zeros((1, 1, 4), dtype=torch.int32, device=DEV), cnt, ws)
         assert lens.tolist() == [1] and cnt.tolist() == [2]
+
+
+@pytest.mark.parametrize("B,new", [(3, 700), (20, 100), (300, 20)])
+def test_append_where_some_sequences_have_a_bad_page(B, new):
+    """The last page of two sequences is none: they keep their lengths, all others get their rows."""
+    old, page, Hkv, d = 10, 16, 2, 64
+    pages = (old + new + page - 1) // page
+    p = P.make_paged_params(B, 4, Hkv, d, page, B * pages, pages, B * new, new, F32, 0.1)
+    table = torch.randperm(B * pages, generator=torch.Generator().manual_seed(B), dtype=torch.int64).to(torch.int32).view(B, pages)
+    bad = {1: -1, B - 1: B * pages}
+    given = table.clone()
+    for b, x in bad.items():
+        given[b, pages - 1] = x
+    K = torch.full((B * pages, Hkv, page, d), 5.0, device=DEV)
+    V, k, v = K.clone(), torch.randn(B * new, Hkv, d, device=DEV), torch.randn(B * new, Hkv, d, device=DEV)
+    lens = torch.full((B,), old, dtype=torch.int32, device=DEV)
+    seen = lens.clone()
+    ws = P.alloc_paged_workspace(p, DEV)
+    cu = torch.arange(0, B * new + 1, new, dtype=torch.int32, device=DEV)
+    P.caote_paged_append(p, K, V, None, None, given.to(DEV), lens, seen, k, v, None, cu, ws)
+    assert P.caote_read_status(ws) == C.ERR_BAD_PAGE
+    want = [old if b in bad else old + new for b in range(B)]
+    assert lens.tolist() == want and seen.tolist() == want
+    for pool, rows in ((K, k), (V, v)):
+        # [B, slots, Hkv, d]
+        got = pool[table.long().to(DEV)].permute(0, 1, 3, 2, 4).reshape(B, pages * page, Hkv, d)
+        assert (got[:, :old] == 5.0).all() and (got[:, old + new:] == 5.0).all()
+        good = [b for b in range(B) if b not in bad]
+        assert torch.equal(got[good, old:old + new], rows.view(B, new, Hkv, d)[good])
