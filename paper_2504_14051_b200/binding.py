@@ -385,6 +385,21 @@ def _pair_stride(fn, k, v):
     return s
 
 
+def check_packed_rows(fn, workspace, q, k, v):
+    """Refuses now what the calls below would refuse about q, k and v [T, heads, d] by and by: for callers that make several."""
+    if workspace.is_cuda:
+        if workspace.get_device() != torch._C._cuda_getDevice():
+            raise ValueError(f"{fn}: the current CUDA device has to be {workspace.device}")
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError(f"{fn}: cannot be captured into a graph")
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        s, (_, heads, d) = _token_stride(fn, name, t), t.shape
+        if t.data_ptr() % 16 or s * t.element_size() % 16 or not heads * d <= s < 1 << 31:
+            raise ValueError(f"{fn}: {name} needs a 16-byte address and a token stride of {heads * d} elements or more, a multiple of "
+                             f"16 bytes; it is at {t.data_ptr():#x} with a stride of {s} elements")
+    _pair_stride(fn, k, v)
+
+
 def caote_prompt_attend(p, q, k, v, cu, o, lse, mass, workspace, stream=None):
     """Causal attention inside packed prompts. lse [T, Hq], mass [T, Hkv]: None if not wanted."""
     fn, io, f32, here = "caote_prompt_attend", _IO.get(p.dtype), torch.float32, torch._C._cuda_getDevice()

@@ -106,7 +106,8 @@ class PagedCache:
 
     A call of `prompt` or `step` takes the new tokens of all sequences packed, q [T, Hq, d], k and v [T, Hkv, d], and how many
     each sequence has (`new`, 0 for none); it returns o [T, Hq, d]. `o` and `lse` of a call are overwritten by the next one. All work
-    goes to the current stream.
+    goes to the current stream. The host's lengths and pages move on with every call, so a captured graph cannot hold one. What is wrong
+    with a call's arguments is found before anything of it runs: a refused call may be repeated.
     """
 
     def __init__(self, batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_tokens, max_total_new, dtype, budget,
@@ -126,6 +127,9 @@ class PagedCache:
         self.n_seen = torch.zeros((batch,), dtype=torch.int32, device=dev)
         self.n_evict = torch.zeros((batch,), dtype=torch.int32, device=dev)
         self.budgets = [budget] * batch if isinstance(budget, int) else [int(x) for x in budget]
+        if len(self.budgets) != batch or sinks < 0 or recent < 0:
+            raise ValueError(f"PagedCache: {batch} budgets, sinks and recent of at least 0 are needed, "
+                             f"not {len(self.budgets)}, {sinks} and {recent}")
         self.budget = torch.tensor(self.budgets, dtype=torch.int32, device=dev)
         self.max_total_new = max_total_new
         self.evict_idx = torch.zeros((batch, n_kv_heads, max_total_new), dtype=torch.int32, device=dev)
@@ -146,11 +150,12 @@ class PagedCache:
         new = [int(m) for m in new]
         T = sum(new)
         for name, t, heads in (("q", q, self.Hq), ("k", k, self.Hkv), ("v", v, self.Hkv)):
-            if t.shape != (T, heads, self.d) or t.dtype is not self.dtype or t.device.type != self.device.type:
-                raise ValueError(f"PagedCache: {name} has to be {(T, heads, self.d)}, {self.dtype} on {self.device}, "
+            if t.shape != (T, heads, self.d) or t.dtype is not self.dtype or t.device != self.K.device:
+                raise ValueError(f"PagedCache: {name} has to be {(T, heads, self.d)}, {self.dtype} on {self.K.device}, "
                                  f"not {tuple(t.shape)}, {t.dtype} on {t.device}")
         if len(new) != self.batch or min(new) < 0 or not 1 <= T <= self.max_total_new:
             raise ValueError(f"PagedCache: {self.batch} sequences with 1 to {self.max_total_new} new tokens together, not {new}")
+        C.check_packed_rows("PagedCache", self.workspace, q, k, v)
         need = [-(-(n + m) // self.page_size) for n, m in zip(self.host_lens, new)]
         if max(need) > self.max_pages:
             raise ValueError(f"PagedCache: a sequence would need {max(need)} pages of at most {self.max_pages}")
