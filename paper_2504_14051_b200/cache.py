@@ -139,6 +139,7 @@ class PagedCache:
         self.workspace = C.alloc_paged_workspace(self._params(max_total_new, max_total_new), dev)
         self.host_lens = [0] * batch
         self._pages = [[] for _ in range(batch)]
+        self._written = [0] * batch  # entries of the device's table that name a page
         self._free = list(range(n_pages - 1, -1, -1))
 
     def _params(self, total, most):
@@ -165,7 +166,11 @@ class PagedCache:
         for b, x in enumerate(more):
             if x:
                 self._pages[b] += [self._free.pop() for _ in range(x)]
-                self.page_table[b, :len(self._pages[b])] = torch.tensor(self._pages[b], dtype=torch.int32)
+            held = len(self._pages[b])
+            if x or held < self._written[b]:  # (entries of pages that came free go: none may name another sequence's page)
+                row = self._pages[b] + [-1] * (self._written[b] - held)
+                self.page_table[b, :len(row)] = torch.tensor(row, dtype=torch.int32)
+                self._written[b] = held
         cu = [0]
         for m in new:
             cu.append(cu[-1] + m)

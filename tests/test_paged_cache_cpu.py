@@ -1,5 +1,5 @@
-"""PagedCache without a GPU: a call that is refused has changed nothing. The library is replaced by one that writes down what it
-was asked for."""
+"""PagedCache without a GPU: a call that is refused has changed nothing, and no entry of the table names a page that its sequence
+does not hold. The library is replaced by one that writes down what it was asked for."""
 import pytest
 import torch
 
@@ -105,3 +105,26 @@ def test_settings_that_an_eviction_would_refuse(calls, bad):
     """... after the tokens are in the pages."""
     with pytest.raises(ValueError):
         cache(**bad)
+
+
+def test_no_entry_names_a_page_of_another_sequence(calls):
+    c = cache()
+    g = torch.Generator().manual_seed(0)
+
+    def check():
+        held = {p: b for b in range(3) for p in c._pages[b]}
+        assert sorted(list(held) + c._free) == list(range(12))
+        for b, row in enumerate(c.page_table.tolist()):
+            assert row[:len(c._pages[b])] == c._pages[b]
+            assert all(held.get(p, b) == b for p in row if p >= 0), (b, row)
+
+    c.prompt(rows(100, Hq), rows(100, Hkv), rows(100, Hkv), [60, 30, 10])
+    check()
+    for i in range(200):
+        if i % 20 == 19:
+            c.release(i // 20 % 3)
+        new = torch.randint(0, 30, (3,), generator=g).tolist()
+        T = max(1, sum(new))
+        new[0] += T - sum(new)
+        c.step(rows(T, Hq), rows(T, Hkv), rows(T, Hkv), new)
+        check()
