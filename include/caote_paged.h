@@ -29,7 +29,7 @@
  * What only the device can see goes to the workspace's status word (caote_read_status): CAOTE_ERR_BAD_LENGTH (cu not
  * ascending or outside [0, T], more than max_new new tokens, len outside [new tokens, max_pages * page_size]; the sequence
  * is skipped), CAOTE_ERR_BAD_PAGE (a page index outside [0, n_pages); nothing is read or written out of bounds; attend: the
- * outputs of that sequence mean nothing, append: the sequence keeps its length, evict: it is skipped),
+ * outputs of that sequence and what its own tokens' weights grow by mean nothing, append: the sequence keeps its length, evict: it is skipped),
  * CAOTE_ERR_OVERFLOW as in caote.h.
  */
 #ifndef CAOTE_PAGED_H_

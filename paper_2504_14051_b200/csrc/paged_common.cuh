@@ -127,6 +127,16 @@ __device__ __forceinline__ size_t pool_row(const PDims& dm, const Seqs& sq, int 
   return (((size_t)page * dm.Hkv + h) << dm.page_shift) + (j & ((1 << dm.page_shift) - 1));
 }
 
+// Where the weight of that token is kept, to be written: null where the page lies outside the pool (page 0 is another sequence's).
+__device__ __forceinline__ float* pool_weight(const PDims& dm, const Seqs& sq, int b, int h, int j, float* mass, int* status) {
+  const int page = __ldg(sq.table + (size_t)b * dm.max_pages + (j >> dm.page_shift));
+  if ((unsigned)page >= (unsigned)dm.n_pages) {
+    set_status(status, CAOTE_ERR_BAD_PAGE);
+    return nullptr;
+  }
+  return mass + ((((size_t)page * dm.Hkv + h) << dm.page_shift) + (j & ((1 << dm.page_shift) - 1)));
+}
+
 // Splits of a sequence's key tiles (device and combine kernel agree on it): `per` tiles each, `count` of them.
 __device__ __forceinline__ void key_splits(int tiles, int most, int least_tiles, int& per, int& count) {
   int ns = tiles / least_tiles;

@@ -416,8 +416,8 @@ finish_kernel(PDims dm, Seqs sq, Records rec, int workers, __nv_bfloat16* __rest
   for (int i = 0; i < kChunk / kFinishThreads; ++i) {
     const int j = j0 + i * kFinishThreads + tid;
     if (j >= s.n) break;
-    float* out = mass + pool_row(dm, sq, b, h, j, status);
-    const float before = *out;
+    float* out = pool_weight(dm, sq, b, h, j, mass, status);
+    const float before = out ? *out : 0.f;
     const float4* src = reinterpret_cast<const float4*>(rec.logits + ((size_t)pair * rec.slots + j) * kRows);
     float sum = 0.f;
 #pragma unroll
@@ -429,7 +429,7 @@ finish_kernel(PDims dm, Seqs sq, Records rec, int workers, __nv_bfloat16* __rest
       if (4 * e + 2 < R) sum += ptx::fast_exp2(x.z - s_stat[4 * e + 2]);
       if (4 * e + 3 < R) sum += ptx::fast_exp2(x.w - s_stat[4 * e + 3]);
     }
-    *out = before + sum;
+    if (out) *out = before + sum;
   }
 }
 

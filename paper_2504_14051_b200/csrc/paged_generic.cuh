@@ -342,8 +342,11 @@ mass_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ K,
     float v = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) v += sums[i * kP + tid];
-    if (kPaged) mass[pool_row(dm, sq, b, h, j0 + tid, status)] += v;
-    else mass[(size_t)(s.t0 + j0 + tid) * dm.Hkv + h] = v;
+    if (kPaged) {
+      if (float* out = pool_weight(dm, sq, b, h, j0 + tid, mass, status)) *out += v;
+    } else {
+      mass[(size_t)(s.t0 + j0 + tid) * dm.Hkv + h] = v;
+    }
   }
 }
 

@@ -788,8 +788,8 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       float before = 0.f;
       if (rh == 0 && j < x.s.n) {
         if (kPaged) {
-          out = mass + pool_row(dm, sq, x.b, x.h, j, status);
-          before = *out;
+          out = pool_weight(dm, sq, x.b, x.h, j, mass, status);
+          if (out) before = *out;
         } else {
           out = mass + ((size_t)x.chunk * dm.T + x.s.t0 + j) * dm.Hkv + x.h;
         }

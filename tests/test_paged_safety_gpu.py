@@ -1,0 +1,55 @@
+"""Calls with page tables or starts that do not fit: what belongs to other sequences stays as it is."""
+import pytest
+import torch
+
+import paper_2504_14051_b200 as P
+from paper_2504_14051_b200 import binding as C
+from test_paged_gpu import BF, DEV, F32, Pages
+
+pytestmark = pytest.mark.gpu
+
+
+def pages_with_page_0_in(b, *args, **kw):
+    """Pages whose page 0, where a bad index might end up, holds the first tokens of sequence b."""
+    pg = Pages(*args, **kw)
+    x = int(pg.table[b, 0])
+    for pool in (pg.K, pg.V, pg.mass):
+        pool[[0, x]] = pool[[x, 0]].clone()
+    zero = pg.table == 0
+    pg.table[pg.table == x] = 0
+    pg.table[zero] = x
+    return pg
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 3, 70])
+def test_a_bad_page_adds_no_weight_to_other_sequences(new, d, dtype):
+    lens = [100, 390, 120]
+    pg = pages_with_page_0_in(0, lens, 2, d, 16, dtype, seed=1)
+    T = 3 * new
+    q = torch.randn(T, 4, d, generator=pg.g).to(dtype).to(DEV)
+    p = P.make_paged_params(3, 4, 2, d, 16, pg.n_pages, pg.max_pages, T, new, dtype, 0.1)
+    ws = P.alloc_paged_workspace(p, DEV)
+    K, V, lens_t = pg.K.to(DEV), pg.V.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV)
+    cu = torch.tensor([0, new, 2 * new, T], dtype=torch.int32, device=DEV)
+
+    def call(table):
+        m, o = pg.mass.to(DEV), torch.zeros((T, 4, d), dtype=dtype, device=DEV)
+        P.caote_paged_attend(p, q, K, V, m, table.to(DEV), lens_t, cu, o, None, ws)
+        return m.cpu().view(torch.int32), o, P.caote_read_status(ws)
+
+    want, o0, st = call(pg.table)
+    assert st == 0
+    own = torch.zeros(pg.n_pages, dtype=torch.bool)
+    own[pg.table[1, :-(-390 // 16)].long()] = True
+    for at in ([2], [0], [24], [3, 7, 20], list(range(25))):
+        for bad in (-1, pg.n_pages, 1 << 30, -(1 << 31)):
+            table = pg.table.clone()
+            table[1, at] = bad
+            got, o, st = call(table)
+            assert st == C.ERR_BAD_PAGE
+            assert torch.equal(got[~own], want[~own]), (at, bad)
+            lost = pg.table[1, at].long()  # the pages whose place the bad index has
+            assert torch.equal(got[lost], pg.mass[lost].view(torch.int32))
+            assert torch.equal(o[:new], o0[:new]) and torch.equal(o[2 * new:], o0[2 * new:])
