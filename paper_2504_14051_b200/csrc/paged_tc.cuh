@@ -14,6 +14,9 @@
 // is a weighted sum, is rounded to bf16 itself, so o's error against 64 bits is sqrt(2) of what the output's type costs.
 // Maximum, sum, O, lse and mass are fp32; the sum takes the numerators before they are rounded.
 //
+// A row that sees a NaN or a logit of +inf is NaN, and so are its statistic and the weights that it gives; a masked weight is
+// exactly 0. Where a row sees none of a split's keys, its statistic there is -inf, and the merge leaves the split out.
+//
 // Operands come by TMA as boxes of 64 channels with the 128-byte swizzle: of q a box of all heads of the group x 128 / G tokens,
 // of K and V a box per page (pages of 16 tokens: eight per tile), by the lanes of a warp side by side. Every mbarrier wait is
 // bounded; one that runs out records CAOTE_ERR_TIMEOUT and the thread carries on in bounds.
@@ -337,7 +340,7 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale22, neg2);
-            const float2 p = e % kPolyOf == kPolyOf - 1 ? poly_exp2x2(x) : make_float2(ptx::fast_exp2(x.x), ptx::fast_exp2(x.y));
+            const float2 p = e % kPolyOf == kPolyOf - 1 ? poly_exp2x2(x, -127.f) : make_float2(ptx::fast_exp2(x.x), ptx::fast_exp2(x.y));
             ls[e & 1] = __fadd2_rn(ls[e & 1], p);
             pk[e] = pack_bf16(p.x, p.y);
           }
@@ -345,9 +348,11 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 #pragma unroll
           for (int e = 0; e < 32; e += 8)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) pm[f] = fmaxf(fmaxf(pm[f], __uint_as_float(v[e + f])), __uint_as_float(v[e + f + 4]));
-          const float mx = fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])) * scale2;
+            for (int f = 0; f < 4; ++f) pm[f] = ptx::max3_nan(pm[f], __uint_as_float(v[e + f]), __uint_as_float(v[e + f + 4]));
+          const float mx = ptx::max3_nan(ptx::max3_nan(pm[0], pm[1], pm[2]), pm[3], pm[3]) * scale2;
           sum = __fadd2_rn(ls[0], ls[1]);
+          // (a NaN or +inf among the keys whose exponentials are polynomials, which do not hand it on)
+          if (!(mx < INFINITY)) sum.x = NAN;
           if (!any_of_pair(mx > m_ref + kMark)) break;
           const float both = row_max(mx);
           float corr = 1.f;
@@ -397,7 +402,8 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
       if (hf == 1) l = *at;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f, stat = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
+    // (l is 0 where the row sees nothing but logits of -inf: none of this split's keys, or a softmax that is no number; NaN goes on)
+    const float inv = 1.f / l, stat = m_ref + __log2f(l);
     char* mine = Qs + i * kTB + (warp & 3) * (kTB / 4);  // the pair's 32 rows
     auto place = [&](int r, int piece) { return mine + r * (kTB / 128) + ((piece ^ (r & 7)) << 4); };
     if (count == 1) {
@@ -494,11 +500,12 @@ combine_kernel(PDims dm, Seqs sq, __nv_bfloat16* __restrict__ o, float* __restri
   float4 v[kR];
 #pragma unroll
   for (int e = 0; e < kR; ++e) {
+    // (the maximum leaves NaN out, the sum does not; nothing but -inf: 0 / 0)
     const float top = warp_max(mine[e]);
-    mine[e] = top == -INFINITY ? 0.f : ptx::fast_exp2(mine[e] - top);
+    mine[e] = mine[e] == -INFINITY ? 0.f : ptx::fast_exp2(mine[e] - top);
     const float sum = warp_sum(mine[e]);
     stat[e] = top + __log2f(sum);
-    mine[e] = sum > 0.f ? mine[e] / sum : 0.f;
+    mine[e] = mine[e] / sum;
     v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
 #pragma unroll 4
@@ -506,8 +513,8 @@ combine_kernel(PDims dm, Seqs sq, __nv_bfloat16* __restrict__ o, float* __restri
     const int sp = s0 + sp0;
 #pragma unroll
     for (int e = 0; e < kR; ++e) {
-      const float w = __shfl_sync(0xffffffffu, mine[e], min(sp, 31));  // (0 behind the last split)
-      if (w > 0.f) {  // (a split in which the row sees no key has written no output)
+      const float w = __shfl_sync(0xffffffffu, mine[e], min(sp, 31));
+      if (w != 0.f && sp < count) {  // (a split in which the row sees no key has written no output)
         const int row = row0 + e;
         const float4 x = *reinterpret_cast<const float4*>(
             opart + ((base + (size_t)sp * (2 * kTile)) * 4 + qu * kTile + row) * kQ + ((piece ^ (row & (kPieces - 1))) << 2));
@@ -570,7 +577,7 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[16], const float
       if (4 * k + 3 < lo || 4 * k + 3 >= hi) b.y = -INFINITY;
     }
     acc[0] = __fadd2_rn(acc[0], make_float2(ptx::fast_exp2(a.x), ptx::fast_exp2(a.y)));
-    if (k & 1) b = poly_exp2x2(b);
+    if (k & 1) b = poly_exp2x2<true>(b, -127.f);
     else b = make_float2(ptx::fast_exp2(b.x), ptx::fast_exp2(b.y));
     acc[1] = __fadd2_rn(acc[1], b);
   }

@@ -211,13 +211,16 @@ __host__ __device__ constexpr uint32_t instr_desc_n(bool b_mn_major, uint32_t n)
 
 // 2^x for two arguments at once on the FMA pipe instead of the special-function unit: x = i + f with i the nearest
 // integer (taken from the low bits of x + 1.5 * 2^23), 2^f on [-1/2, 1/2] by a polynomial of degree 4 that is exact at
-// f = 0 (relative error below 3e-6), and i added to the exponent field. Arguments below -126 give about 2^-126.
+// f = 0 (relative error below 3e-6), and i added to the exponent field. Arguments below `least`, NaN among them, count as `least`:
+// -126 gives 2^-126, -127 gives 0.
 // The score pass is bound by the special-function unit's 16 results per clock and SM (one exponential per
 // (row, key) pair); it hands a quarter of them to this routine.
-__device__ __forceinline__ float2 poly_exp2x2(float2 x) {
+// kNan: NaN stays NaN instead (a multiplication more).
+template <bool kNan = false>
+__device__ __forceinline__ float2 poly_exp2x2(float2 x, float least = -126.f) {
   constexpr float kMagic = 12582912.f;
-  x.x = fmaxf(x.x, -126.f);
-  x.y = fmaxf(x.y, -126.f);
+  x.x = kNan ? ptx::max3_nan(x.x, least, least) : fmaxf(x.x, least);
+  x.y = kNan ? ptx::max3_nan(x.y, least, least) : fmaxf(x.y, least);
   const float2 t = __fadd2_rn(x, make_float2(kMagic, kMagic));
   const float2 r = __fadd2_rn(t, make_float2(-kMagic, -kMagic));
   const float2 f = __ffma2_rn(r, make_float2(-1.f, -1.f), x);
@@ -226,6 +229,8 @@ __device__ __forceinline__ float2 poly_exp2x2(float2 x) {
   p = __ffma2_rn(p, f, make_float2(0.24023915827274323f, 0.24023915827274323f));
   p = __ffma2_rn(p, f, make_float2(0.6931241154670715f, 0.6931241154670715f));
   p = __ffma2_rn(p, f, make_float2(1.f, 1.f));
+  if (kNan)  // (2^i as a factor: added to the exponent of a NaN it would make a number)
+    return __fmul2_rn(p, make_float2(__int_as_float(0x3f800000 + (__float_as_int(t.x) << 23)), __int_as_float(0x3f800000 + (__float_as_int(t.y) << 23))));
   return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
                      __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
