@@ -16,7 +16,8 @@
 //                   that the decode kernel left in the workspace (8 NT floats per slot beside the 4 D bytes read: reading K a
 //                   second time would be 2 D).
 //
-// P is rounded to bf16 for its product, as in paged_tc.cuh; everything that is summed or carried is fp32.
+// P is rounded to bf16 for its product, as in paged_tc.cuh; everything that is summed or carried is fp32. NaN and logits of +inf make
+// a row, its statistic and its weights NaN, as there.
 #pragma once
 
 #include <cuda.h>
@@ -228,8 +229,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         float sum = l[t][e];
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        inv[e] = sum > 0.f ? 1.f / sum : 0.f;
-        if (oct == 0) rec.stat[slot * kRows + 8 * t + 2 * quad + e] = sum > 0.f ? ref[t][e] + __log2f(sum) : -INFINITY;
+        // (0: the row sees none of this part's tokens, or logits of -inf alone; NaN goes on)
+        inv[e] = sum == 0.f ? 0.f : 1.f / sum;
+        if (oct == 0) rec.stat[slot * kRows + 8 * t + 2 * quad + e] = sum == 0.f ? -INFINITY : ref[t][e] + __log2f(sum);
       }
       float* dst = rec.o + (slot * kRows + 8 * t + 2 * quad) * D + oct;
 #pragma unroll
@@ -370,9 +372,11 @@ finish_kernel(PDims dm, Seqs sq, Records rec, int workers, __nv_bfloat16* __rest
     for (int i = e; i < n_rec; i += 16) mx = fmaxf(mx, rec.stat[(slot + i) * kRows + r]);
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-    float sum = 0.f;
-    if (mx != -INFINITY)
-      for (int i = e; i < n_rec; i += 16) sum += ptx::fast_exp2(rec.stat[(slot + i) * kRows + r] - mx);
+    float sum = 0.f;  // (the maximum leaves NaN out, the sum does not)
+    for (int i = e; i < n_rec; i += 16) {
+      const float x = rec.stat[(slot + i) * kRows + r];
+      sum += x == -INFINITY ? 0.f : ptx::fast_exp2(x - mx);
+    }
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
     if (e == 0) s_stat[r] = mx + __log2f(sum);
@@ -420,14 +424,19 @@ finish_kernel(PDims dm, Seqs sq, Records rec, int workers, __nv_bfloat16* __rest
     const float before = out ? *out : 0.f;
     const float4* src = reinterpret_cast<const float4*>(rec.logits + ((size_t)pair * rec.slots + j) * kRows);
     float sum = 0.f;
+    if (j <= s.n - s.m) {
 #pragma unroll
-    for (int e = 0; e < kRows / 4; ++e) {
-      if (4 * e >= R) break;
-      const float4 x = src[e];
-      sum += ptx::fast_exp2(x.x - s_stat[4 * e]);
-      if (4 * e + 1 < R) sum += ptx::fast_exp2(x.y - s_stat[4 * e + 1]);
-      if (4 * e + 2 < R) sum += ptx::fast_exp2(x.z - s_stat[4 * e + 2]);
-      if (4 * e + 3 < R) sum += ptx::fast_exp2(x.w - s_stat[4 * e + 3]);
+      for (int e = 0; e < kRows / 4; ++e) {
+        if (4 * e >= R) break;
+        const float4 x = src[e];
+        sum += ptx::fast_exp2(x.x - s_stat[4 * e]);
+        if (4 * e + 1 < R) sum += ptx::fast_exp2(x.y - s_stat[4 * e + 1]);
+        if (4 * e + 2 < R) sum += ptx::fast_exp2(x.z - s_stat[4 * e + 2]);
+        if (4 * e + 3 < R) sum += ptx::fast_exp2(x.w - s_stat[4 * e + 3]);
+      }
+    } else {  // (new tokens, but the first: the rows before them have nothing to say, even if they are NaN)
+#pragma unroll 1
+      for (int r = (j - (s.n - s.m)) * dm.G; r < R; ++r) sum += ptx::fast_exp2(reinterpret_cast<const float*>(src)[r] - s_stat[r]);
     }
     if (out) *out = before + sum;
   }

@@ -172,6 +172,22 @@ def test_a_query_over_the_pages(lens, new, dtype, d):
     query_over_the_pages(lens, new, dtype, d)
 
 
+FEW = [([700, 90], [1, 1]), ([700, 90], [3, 2]), ([3000], [1]), ([1200], [8])]
+
+
+@pytest.mark.parametrize("dtype,d", FORMS)
+@pytest.mark.parametrize("value", KEYS)
+@pytest.mark.parametrize("lens,new", FEW)
+def test_a_key_in_the_pages_of_few_rows(lens, new, value, dtype, d):
+    key_in_the_pages(lens, new, KEYS[value], dtype, d)
+
+
+@pytest.mark.parametrize("dtype,d", FORMS)
+@pytest.mark.parametrize("lens,new", FEW)
+def test_a_query_of_few_rows(lens, new, dtype, d):
+    query_over_the_pages(lens, new, dtype, d)
+
+
 @pytest.mark.parametrize("dtype,d", FORMS)
 def test_large_values_of_tokens_that_a_row_does_not_see(dtype, d):
     """A masked weight is exactly 0."""
