@@ -208,7 +208,8 @@ attend_kernel(PDims dm, Seqs sq, const T* __restrict__ q, const T* __restrict__ 
     const int row = r0 + ty * RPT + r;
     if (row >= R) continue;
     const size_t at = (size_t)(s.t0 + row / dm.G) * dm.Hq + h * dm.G + row % dm.G;  // the row's place in lse and o
-    const float inv = l[r] > 0.f ? 1.f / l[r] : 0.f, stat = top[r] + __log2f(l[r]);  // (no key in this split: -inf)
+    // (l is 0 where the row sees no key of this split, which the merge leaves out, or logits of -inf alone: no number)
+    const float inv = 1.f / l[r], stat = top[r] + __log2f(l[r]);
     if (count == 1) {
       if (tx == 0) {
         lse2[stat_at(dm, s, h, row)] = stat;

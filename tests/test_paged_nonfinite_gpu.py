@@ -189,6 +189,22 @@ def test_a_query_of_few_rows(lens, new, dtype, d):
 
 
 @pytest.mark.parametrize("dtype,d", FORMS)
+@pytest.mark.parametrize("n,m", [(300, 1), (3000, 1), (300, 300), (3000, 70)])
+def test_logits_of_minus_infinity_alone(n, m, dtype, d):
+    """A softmax over nothing but -inf is no number (nor is one over NaN: the second head, 0 times an infinity)."""
+    pg = Pages([n], 1, d, 16, dtype, seed=4)
+    pg.K[:, :, :, 0] = -INF
+    q = torch.randn(m, 2, d, generator=pg.g)
+    q[:, 0, 0], q[:, 1, 0] = 1.0, 0.0
+    q[:, 1] = 0.0
+    o, lse = torch.zeros((m, 2, d), dtype=dtype, device=DEV), torch.zeros((m, 2), device=DEV)
+    p = P.make_paged_params(1, 2, 1, d, 16, pg.n_pages, pg.max_pages, m, m, dtype, 0.1)
+    P.caote_paged_attend(p, q.to(dtype).to(DEV), pg.K.to(DEV), pg.V.to(DEV), None, pg.table.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV),
+                         torch.tensor([0, m], dtype=torch.int32, device=DEV), o, lse, P.alloc_paged_workspace(p, DEV))
+    assert torch.isnan(o).all()
+
+
+@pytest.mark.parametrize("dtype,d", FORMS)
 def test_large_values_of_tokens_that_a_row_does_not_see(dtype, d):
     """A masked weight is exactly 0."""
     g = torch.Generator().manual_seed(6)
