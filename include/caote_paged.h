@@ -20,6 +20,9 @@
  *   page_table   [B, max_pages]     int32: slot j of sequence b lies in page page_table[b, j / page_size]. Entries behind a
  *                                   sequence's length are not read.
  *   len, n_seen, budget, n_evict [B] int32: tokens in the cache, tokens ever appended, tokens to keep, tokens evicted
+ * Values: weighted values are summed in fp32, with weights of up to 2^20 in bf16 (2^0 in fp32) before they are divided by their sum, so
+ * |v| n has to stay below 2^107 (2^127). A row that sees a NaN or a logit of +inf is NaN in o and lse, and so are the weights that it
+ * gives; a row all of whose logits are -inf is NaN in o. A NaN or infinity in v may also reach the rows of the tokens before it.
  * Outputs must not overlap inputs. Strides in elements, 0 = dense; q, k and v may be slices of one buffer. q, k, v, K, V, o must be 16-byte aligned, and so
  * must their strides in bytes; the other arrays 4-byte aligned.
  *

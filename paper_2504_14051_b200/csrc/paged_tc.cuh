@@ -284,11 +284,11 @@ attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           : "=r"(r) : "r"((uint32_t)x), "r"(pair_bar) : "memory");
       return r != 0;
     };
-    // Numerators are 2^(logit - m_ref) for a reference that is left alone until a logit passes it by 2^60: nothing is lost meanwhile
+    // Numerators are 2^(logit - m_ref) for a reference that is left alone until a logit passes it by 20: nothing is lost meanwhile
     // (P, l and O are floats, their ratios do not depend on it), and no maximum stands between a logit and its exponential. The
     // 32 keys of a part are exponentiated and their maximum is formed at the same time; only where it has passed the mark is the
-    // part done again, with a new reference.
-    constexpr float kMark = 60.f;
+    // part done again, with a new reference. (O holds up to 2^20 n times the values: with a mark of 60 those beyond 2^67 / n overflowed.)
+    constexpr float kMark = 20.f;
     float m_ref = -INFINITY, l = 0.f;
     const float2 scale22 = make_float2(scale2, scale2);
     for (int kt = 0; kt < c; ++kt) {

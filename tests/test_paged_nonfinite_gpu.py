@@ -204,6 +204,21 @@ def test_logits_of_minus_infinity_alone(n, m, dtype, d):
     assert torch.isnan(o).all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [40, 70, 110, 130, 200, 250])
+def test_large_values_behind_rising_logits(at, d):
+    """Numerators are formed against a reference that may lag: values of up to 2^80 times these are still in range."""
+    g = torch.Generator().manual_seed(5)
+    T = 300
+    q = torch.ones(T, 4, d).to(BF)
+    k, v = (0.05 * torch.randn(T, 2, d, generator=g)).to(BF), (2.0 ** 80 * (torch.rand(T, 2, d, generator=g) * 2 - 1)).to(BF)
+    for rise in (10.0, 14.5, 20.0, 40.0, 60.0):  # (nats)
+        x = k.clone()
+        x[at] = rise / d
+        x[at + 20] = 1.4 * rise / d
+        prompt(q, x, v, [T], BF, 1.0)
+
+
 @pytest.mark.parametrize("dtype,d", FORMS)
 def test_large_values_of_tokens_that_a_row_does_not_see(dtype, d):
     """A masked weight is exactly 0."""
