@@ -29,9 +29,9 @@
  * Calls that write pages (append, evict, attend with mass) need pages that belong to one sequence each. Calls that only read
  * them do not: sequences may share pages.
  *
- * What only the device can see goes to the workspace's status word (caote_read_status): CAOTE_ERR_BAD_LENGTH (cu not
- * ascending or outside [0, T], more than max_new new tokens, len outside [new tokens, max_pages * page_size]; the sequence
- * is skipped), CAOTE_ERR_BAD_PAGE (a page index outside [0, n_pages); nothing is read or written out of bounds; attend: the
+ * What only the device can see goes to the workspace's status word (caote_read_status): CAOTE_ERR_BAD_LENGTH (cu outside
+ * [0, T], more than max_new new tokens, len outside [new tokens, max_pages * page_size]: the sequence is skipped; cu not ascending:
+ * append moves no length on, the other calls' outputs mean nothing), CAOTE_ERR_BAD_PAGE (a page index outside [0, n_pages); nothing is read or written out of bounds; attend: the
  * outputs of that sequence and what its own tokens' weights grow by mean nothing, append: the sequence keeps its length, evict: it is skipped),
  * CAOTE_ERR_OVERFLOW as in caote.h.
  */

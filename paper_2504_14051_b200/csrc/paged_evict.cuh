@@ -20,7 +20,8 @@ constexpr int kEvictThreads = sel::kSelThreads;
 constexpr unsigned kSheltered = 0xffffffffu;  // as the score bits of a sheltered token: behind every other
 
 // New rows into the pages: a thread per 16 bytes of a K or V row, the pieces of a token side by side. The CTA that finishes last moves
-// the lengths on; a sequence that does not fit, or one of whose pages is none, keeps its length. Up to as many CTAs as are resident at
+// the lengths on; a sequence that does not fit, or one of whose pages is none, keeps its length, and all do where cu does not ascend (the
+// search for a row's sequence means nothing then). Up to as many CTAs as are resident at
 // once: more would wait for their turn (8 sequences of 512 tokens, 8 KV heads, 16.8 MB, cold: 20.5 us with five per SM, 19 with six, 20
 // with eight, whose 32 registers do not suffice; two and four tokens on their way per thread: 1 and 5 us longer).
 constexpr int kAppendThreads = 256, kAppendCtas = 6, kSharedStarts = 1024;
@@ -88,6 +89,9 @@ append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __re
   __syncthreads();
   if (!s_last) return;
   __threadfence();
+  bool descends = false;
+  for (int b = tid; b < dm.B; b += kAppendThreads) descends |= start(b + 1) < start(b);
+  descends = __syncthreads_or(descends) != 0;
   // (a power of two of lanes per sequence, so that one round of the CTA does where it can: they share the look at its pages)
   int lanes = 32;
   while (lanes > 1 && (long long)lanes * dm.B > kAppendThreads) lanes >>= 1;
@@ -96,7 +100,7 @@ append_kernel(PDims dm, Seqs sq, int row_bytes, long long src_stride, char* __re
     const int b = b0 + tid / lanes;
     const bool there = b < dm.B;
     const int t0 = there ? start(b) : 0, t1 = there ? start(b + 1) : 0, m = t1 - t0, n = there ? len[b] : 0;
-    const bool sound = t0 >= 0 && t1 >= t0 && t1 <= dm.T && m <= dm.max_new && n >= 0, fits = sound && n + (long long)m <= cap;
+    const bool sound = !descends && t0 >= 0 && t1 <= dm.T && m <= dm.max_new && n >= 0, fits = sound && n + (long long)m <= cap;
     bool ok = true;
     if (fits && m > 0) {
 #pragma unroll 4

@@ -53,3 +53,26 @@ def test_a_bad_page_adds_no_weight_to_other_sequences(new, d, dtype):
             lost = pg.table[1, at].long()  # the pages whose place the bad index has
             assert torch.equal(got[lost], pg.mass[lost].view(torch.int32))
             assert torch.equal(o[:new], o0[:new]) and torch.equal(o[2 * new:], o0[2 * new:])
+
+
+@pytest.mark.parametrize("many", [0, 1100])
+@pytest.mark.parametrize("cu", [[0, 5, 3, 8], [4, 8, 0, 4], [0, 0, 4, 2, 8], [0, 8, 7]])
+def test_append_with_starts_that_do_not_ascend(cu, many):
+    """Which sequence a row belongs to is not clear then: no length moves on (with more sequences than fit shared memory, too)."""
+    cu = cu + [8] * many
+    B, T = len(cu) - 1, 8
+    p = P.make_paged_params(B, 2, 1, 64, 16, 2 * B, 2, T, T, F32, 0.1)
+    ws = P.alloc_paged_workspace(p, DEV)
+    K = torch.full((2 * B, 1, 16, 64), 5.0, device=DEV)
+    V, k = K.clone(), torch.randn(T, 1, 64, device=DEV)
+    table = torch.arange(2 * B, dtype=torch.int32, device=DEV).view(B, 2)
+    lens = torch.full((B,), 3, dtype=torch.int32, device=DEV)
+    seen = torch.full((B,), 9, dtype=torch.int32, device=DEV)
+    P.caote_paged_append(p, K, V, None, None, table, lens, seen, k, k, None, torch.tensor(cu, dtype=torch.int32, device=DEV), ws)
+    assert P.caote_read_status(ws) == C.ERR_BAD_LENGTH
+    assert (lens == 3).all() and (seen == 9).all()
+    assert (K[:, :, :3] == 5.0).view(B, 2, -1)[:, 0].all() and (V[:, :, :3] == 5.0).view(B, 2, -1)[:, 0].all()  # the tokens that are there
+    cu = torch.tensor([0, 5, 8] + [8] * (B - 2), dtype=torch.int32, device=DEV)
+    P.caote_paged_append(p, K, V, None, None, table, lens, seen, k, k, None, cu, ws)  # (the workspace is as good as before)
+    assert P.caote_read_status(ws) == 0 and lens[:2].tolist() == [8, 6] and (lens[2:] == 3).all()
+    assert torch.equal(K[0, 0, 3:8], k[:5, 0]) and torch.equal(V[2, 0, 3:6], k[5:, 0])
