@@ -59,7 +59,10 @@ __device__ __forceinline__ Seq sequence(const PDims& dm, const Seqs& sq, int b, 
 __device__ __forceinline__ size_t stat_at(const PDims& dm, const Seq& s, int h, int r) { return ((size_t)h * dm.T + s.t0) * dm.G + r; }
 
 // Work is numbered over all sequences: a sequence has ceil(what / per) blocks of it, what = its new tokens or its keys. A scan holds
-// one sequence per lane (32 at a time); for one whole warp.
+// one sequence per lane (32 at a time); for one whole warp. Sums stop at kMostBlocks: sequences that overlap (cu does not ascend) may have
+// any number of blocks together, those of a sound call have less. Which block of its sequence an index is stays in range all the same.
+constexpr unsigned kMostBlocks = 0x7fff0000u;
+__device__ __forceinline__ int add_blocks(int a, int b) { return (int)min((unsigned)a + (unsigned)b, kMostBlocks); }
 struct Scan {
   Seq s;           // this lane's sequence
   int mine, incl;  // its blocks, and those of all lanes up to it
@@ -76,7 +79,7 @@ __device__ __forceinline__ Scan scan(const PDims& dm, const Seqs& sq, int b0, in
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int t = __shfl_up_sync(0xffffffffu, c.incl, o);
-    if (lane >= o) c.incl += t;
+    if (lane >= o) c.incl = add_blocks(c.incl, t);
   }
   c.total = __shfl_sync(0xffffffffu, c.incl, 31);
   return c;
@@ -86,7 +89,7 @@ template <typename What>
 __device__ __forceinline__ int count_blocks(const PDims& dm, const Seqs& sq, int per, What what, int* status, Scan& c) {
   c = scan(dm, sq, 0, per, what, status);
   int total = c.total;
-  for (int b0 = 32; b0 < dm.B; b0 += 32) total += scan(dm, sq, b0, per, what, status).total;
+  for (int b0 = 32; b0 < dm.B; b0 += 32) total = add_blocks(total, scan(dm, sq, b0, per, what, status).total);
   return total;
 }
 // The sequence that block `index` belongs to, and its number in there, from the first scan on; false: no such block. The same

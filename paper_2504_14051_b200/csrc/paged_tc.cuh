@@ -87,7 +87,7 @@ struct Schedule {
 };
 __device__ __forceinline__ Schedule schedule(const PDims& dm, int per_head, int sms, int most_splits) {
   Schedule c;
-  c.items = per_head * dm.Hkv;
+  c.items = (int)min((long long)per_head * dm.Hkv, (long long)kMostBlocks);
   c.whole = c.items / sms * sms;
   c.splits = c.items > c.whole ? min(most_splits, sms / (c.items - c.whole)) : 1;
   return c;

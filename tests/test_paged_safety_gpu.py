@@ -76,3 +76,40 @@ def test_append_with_starts_that_do_not_ascend(cu, many):
     P.caote_paged_append(p, K, V, None, None, table, lens, seen, k, k, None, cu, ws)  # (the workspace is as good as before)
     assert P.caote_read_status(ws) == 0 and lens[:2].tolist() == [8, 6] and (lens[2:] == 3).all()
     assert torch.equal(K[0, 0, 3:8], k[:5, 0]) and torch.equal(V[2, 0, 3:6], k[5:, 0])
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64)])
+@pytest.mark.parametrize("m", [1, 3, 60])
+def test_sequences_that_overlap_are_reported_and_nothing_else_is_touched(m, dtype, d):
+    """cu that goes back and forth: every second sequence has all rows, more row blocks than the call has room for."""
+    B, guard = 66, 7.0
+    cu = torch.tensor([0, m] * (B // 2) + [0], dtype=torch.int32, device=DEV)
+    g = torch.Generator().manual_seed(3)
+
+    def guarded(*shape, dtype):
+        """A tensor in the middle of a larger one."""
+        n = 1
+        for x in shape:
+            n *= x
+        whole = torch.full((n + 2 * 4096,), guard, dtype=dtype, device=DEV)
+        return whole, whole[4096:4096 + n].view(shape)
+
+    q, k, v = (torch.randn(m, h, d, generator=g).to(dtype).to(DEV) for h in (4, 2, 2))
+    pg = Pages([200] * B, 2, d, 16, dtype, seed=3)
+    for pages in (False, True):
+        p = P.make_paged_params(B, 4, 2, d, *((16, pg.n_pages, pg.max_pages) if pages else (0, 0, 0)), m, m, dtype, 0.1)
+        size = C.caote_paged_workspace_bytes(p)
+        space, ws = guarded(size, dtype=torch.uint8)
+        ws.zero_()
+        all_o, o = guarded(m, 4, d, dtype=dtype)
+        all_lse, lse = guarded(m, 4, dtype=F32)
+        if pages:
+            all_mass, mass = guarded(pg.n_pages, 2, 16, dtype=F32)
+            mass.copy_(pg.mass)
+            P.caote_paged_attend(p, q, pg.K.to(DEV), pg.V.to(DEV), mass, pg.table.to(DEV), torch.full((B,), 200, dtype=torch.int32, device=DEV), cu, o, lse, ws)
+        else:
+            all_mass, mass = guarded(m, 2, dtype=F32)
+            P.caote_prompt_attend(p, q, k, v, cu, o, lse, mass, ws)
+        assert P.caote_read_status(ws) == C.ERR_BAD_LENGTH
+        for x in (space, all_o, all_lse, all_mass):
+            assert (x[:4096] == guard).all() and (x[-4096:] == guard).all()
