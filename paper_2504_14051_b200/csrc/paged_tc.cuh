@@ -19,7 +19,8 @@
 //
 // Operands come by TMA as boxes of 64 channels with the 128-byte swizzle: of q a box of all heads of the group x 128 / G tokens,
 // of K and V a box per page (pages of 16 tokens: eight per tile), by the lanes of a warp side by side. Every mbarrier wait is
-// bounded; one that runs out records CAOTE_ERR_TIMEOUT and the thread carries on in bounds.
+// bounded; one that runs out records CAOTE_ERR_TIMEOUT and the thread carries on in bounds, or, where it waited for its next item,
+// comes to its end.
 #pragma once
 
 #include <cuda.h>
@@ -680,7 +681,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       const int buf = c & 1;
       if (c > 0) find_next(draw());
       const Item& x = nx.x;
-      if (c >= 2) mbar_wait_idle(&item_free[buf], ((c >> 1) - 1) & 1, status);
+      if (c >= 2 && !__all_sync(0xffffffffu, mbar_wait_idle(&item_free[buf], ((c >> 1) - 1) & 1, status))) break;
       if (lane == 0) {
         items[buf] = x;
         if (x.b >= 0) mbar_expect_tx(&k_bar[buf], (nx.boxes[0] + nx.boxes[1]) * box * D * 2);  // (also says that the item is there)
@@ -697,7 +698,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     if (ptx::elect_one()) {
       int qb = 0;
       for (int c = 0;; ++c) {
-        mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status);
+        if (!mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status)) break;
         const Item x = items[c & 1];
         if (x.b < 0) break;
         for (int rb = 0; rb < x.blocks; ++rb, ++qb) {
@@ -714,7 +715,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     // =============================== the rows' statistics (the warp) ===============================
     int qb = 0;
     for (int c = 0;; ++c) {
-      mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status);
+      if (!__all_sync(0xffffffffu, mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status))) break;
       const Item x = items[c & 1];
       if (x.b < 0) break;
       const float* src = lse2 + stat_at(dm, x.s, x.h, x.rb0 * tok * dm.G);
@@ -753,7 +754,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       constexpr uint32_t kIdesc = instr_desc_n(false, kTile);
       int qb = 0;
       for (int c = 0;; ++c) {
-        mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status);
+        if (!mbar_wait_idle(&k_bar[c & 1], (c >> 1) & 1, status)) break;
         const int b = items[c & 1].b, blocks = items[c & 1].blocks;
         if (b < 0) break;
         const int tiles = items[c & 1].j0 + kTile < items[c & 1].s.n ? 2 : 1;
@@ -782,9 +783,20 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     const float scale2 = dm.scale * kLog2e;
     const int kk = (warp >> 2) & 1, rh = warp >> 3, key = tid & (kKeys - 1);
     const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kk * 256 + rh * 64;
+    auto all_of_pair = [&](bool x) {
+      uint32_t r;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\t"
+          "setp.ne.u32 q, %1, 0;\n\t"
+          "bar.red.and.pred p, %2, 64, q;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(r) : "r"((uint32_t)x), "r"(1 + (warp & 7)) : "memory");
+      return r != 0;
+    };
     int qb = 0;
     for (int c = 0;; ++c) {
-      mbar_wait(&k_bar[c & 1], (c >> 1) & 1, status);
+      // (the two warps that share 32 keys, which meet below, go on together or not at all)
+      if (!all_of_pair(mbar_wait(&k_bar[c & 1], (c >> 1) & 1, status))) break;
       const Item x = items[c & 1];
       if (x.b < 0) break;
       const int j = x.j0 + key, first = x.s.n - x.s.m;

@@ -25,29 +25,32 @@ using ptx::bulk_load;
 using ptx::fence_async_smem;
 using ptx::fast_exp2;
 using ptx::tile_off;
-// Bounded wait. On expiry the error is recorded and the caller carries on (see the file comment).
-__device__ __forceinline__ void mbar_wait(uint64_t* bar, uint32_t parity, int* status) {
-  if (mbar_try_wait(bar, parity)) return;
+// Bounded wait. On expiry the error is recorded and the answer is false; a caller that has no use for what it waited for leaves,
+// others carry on.
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, int* status) {
+  if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity)) {
     if (clock64() - t0 > kWaitCycles) {
       set_status(status, CAOTE_ERR_TIMEOUT);
-      return;
+      return false;
     }
   }
+  return true;
 }
 // The same for the single-lane helper warps: they back off between polls so that their spinning does
 // not take issue slots from the warps that do the arithmetic on the same scheduler.
-__device__ __forceinline__ void mbar_wait_idle(uint64_t* bar, uint32_t parity, int* status) {
-  if (mbar_try_wait(bar, parity)) return;
+__device__ __forceinline__ bool mbar_wait_idle(uint64_t* bar, uint32_t parity, int* status) {
+  if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity)) {
     __nanosleep(20);
     if (clock64() - t0 > kWaitCycles) {
       set_status(status, CAOTE_ERR_TIMEOUT);
-      return;
+      return false;
     }
   }
+  return true;
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
