@@ -800,7 +800,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       const Item x = items[c & 1];
       if (x.b < 0) break;
       const int j = x.j0 + key, first = x.s.n - x.s.m;
-      const int need = (j - first) * dm.G;  // the first of the pair's rows that sees the key
+      const int need = max(j - first, 0) * dm.G;  // the first of the pair's rows that sees the key (of older keys far less than 0 otherwise)
       // where the sum goes, and what is there already: fetched now, used at the end
       float* out = nullptr;
       float total = 0.f, low = 0.f;  // the sum over row blocks, and what its additions lost

@@ -113,3 +113,24 @@ def test_sequences_that_overlap_are_reported_and_nothing_else_is_touched(m, dtyp
         assert P.caote_read_status(ws) == C.ERR_BAD_LENGTH
         for x in (space, all_o, all_lse, all_mass):
             assert (x[:4096] == guard).all() and (x[-4096:] == guard).all()
+
+
+def test_weights_in_a_cache_of_more_than_2_27_tokens():
+    """Groups of 16: the first row that sees a key, counted from the key's end of the cache, passes 32 bits. All keys are equal, so that
+    sums are whole numbers up to 2^23 and every weight is 16 / (n - 1) + 16 / n: off by the log-sum-exp, 27 in the log2 domain (2^-19
+    there, twice, times ln 2), and the exponential (2^-21)."""
+    n, page, d = (1 << 27) + 1024, 256, 64
+    pages = n // page
+    K = torch.zeros((pages, 1, page, d), dtype=BF, device=DEV)
+    V, mass = torch.zeros_like(K), torch.zeros((pages, 1, page), device=DEV)
+    p = P.make_paged_params(1, 16, 1, d, page, pages, pages, 2, 2, BF, 0.1)
+    ws = P.alloc_paged_workspace(p, DEV)
+    q, o = torch.ones((2, 16, d), dtype=BF, device=DEV), torch.zeros((2, 16, d), dtype=BF, device=DEV)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).view(1, pages)
+    P.caote_paged_attend(p, q, K, V, mass, table, torch.tensor([n], dtype=torch.int32, device=DEV), torch.tensor([0, 2], dtype=torch.int32, device=DEV),
+                         o, None, ws)
+    assert P.caote_read_status(ws) == 0
+    flat = mass.view(-1)
+    want, tol = 16 / (n - 1) + 16 / n, 2 * 0.7 * 2.0 ** -19 + 2.0 ** -21 + 32 * 2.0 ** -24
+    assert ((flat[:-1] - want).abs() <= tol * want).all(), (flat[:-1] - want).abs().argmax()
+    assert abs(float(flat[-1]) - 16 / n) <= tol * 16 / n
