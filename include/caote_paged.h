@@ -51,7 +51,7 @@ typedef struct {
   int32_t head_dim;   /* d in {64, 128}                                                            */
   int32_t page_size;  /* tokens per page: 16, 32, 64, 128 or 256. Prompts alone: 0                 */
   int32_t n_pages;    /* pages in the pool; n_pages * Hkv * page_size < 2^31. Prompts alone: 0     */
-  int32_t max_pages;  /* columns of the page table. Prompts alone: 0                               */
+  int32_t max_pages;  /* columns of the page table, max_pages * page_size <= 2^31 - 2^16; prompts: 0 */
   int32_t total_new;  /* T >= 1, T * G < 2^28                                                      */
   int32_t max_new;    /* most new tokens of one sequence in this call, 1 .. T                      */
   int32_t dtype;      /* caote_dtype_t of q, k, v, K, V, o                                         */

@@ -13,6 +13,8 @@
 namespace caote {
 namespace paged {
 
+// Slots of a sequence: numbers of slots a few blocks and rounds of CTAs behind the last one still fit 32 bits.
+constexpr long long kMostSlots = (1LL << 31) - (1LL << 16);
 static bool params_ok(const caote_paged_params_t* p, bool pages) {
   if (!p) return false;
   if (p->batch < 1 || p->n_kv_heads < 1 || p->n_q_heads < 1 || p->total_new < 1 || p->max_new < 1) return false;
@@ -23,7 +25,7 @@ static bool params_ok(const caote_paged_params_t* p, bool pages) {
     if (p->n_pages < 1 || p->max_pages < 1) return false;
     if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128 && p->page_size != 256) return false;
     if ((long long)p->n_pages * p->n_kv_heads * p->page_size >= (1LL << 31)) return false;
-    if ((long long)p->max_pages * p->page_size >= (1LL << 31)) return false;
+    if ((long long)p->max_pages * p->page_size > kMostSlots) return false;
   }
   return true;
 }
@@ -84,7 +86,7 @@ constexpr int kFewRowsMass = 16, kFewRows = 32;
 static bool few_rows(const PDims& dm, int dtype, bool mass) {
   const long long tiles = ((long long)dm.max_pages << dm.page_shift) / 16 * dm.B * dm.Hkv;  // (at most)
   return dtype == CAOTE_BF16 && dm.max_pages > 0 && dm.scale > 0.f && (long long)dm.max_new * dm.G <= (mass ? kFewRowsMass : kFewRows) &&
-         tiles < (1LL << 31) && dm.B * dm.Hkv <= 65535;
+         tiles <= kMostSlots && dm.B * dm.Hkv <= 65535;
 }
 static int few_workers() { return g_sm_count * few::kWarps; }
 static size_t carve(const PDims& dm, int dtype, char* base, Scratch* out) {
