@@ -134,3 +134,23 @@ def test_weights_in_a_cache_of_more_than_2_27_tokens():
     want, tol = 16 / (n - 1) + 16 / n, 2 * 0.7 * 2.0 ** -19 + 2.0 ** -21 + 32 * 2.0 ** -24
     assert ((flat[:-1] - want).abs() <= tol * want).all(), (flat[:-1] - want).abs().argmax()
     assert abs(float(flat[-1]) - 16 / n) <= tol * 16 / n
+
+
+def test_a_cache_refuses_to_be_captured_and_goes_on():
+    c = P.PagedCache(1, 4, 2, 64, 16, 8, 100, 40, BF, 30)
+    q, k, v = (torch.randn(40, h, 64, device=DEV).to(BF) for h in (4, 2, 2))
+    c.prompt(q, k, v, [40])
+    before = (list(c.host_lens), [list(p) for p in c._pages], c.lens.tolist())
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        try:
+            with pytest.raises(ValueError, match="captured"):
+                c.step(q[:1], k[:1], v[:1], [1])
+        finally:
+            graph.capture_end()
+    torch.cuda.synchronize()
+    assert (list(c.host_lens), [list(p) for p in c._pages], c.lens.tolist()) == before
+    c.step(q[:1], k[:1], v[:1], [1])
+    assert c.lens.tolist() == c.host_lens == [30] and c.status() == 0
