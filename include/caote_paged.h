@@ -23,17 +23,17 @@
  * Values: weighted values are summed in fp32, with weights of up to 2^20 in bf16 (2^0 in fp32) before they are divided by their sum, so
  * |v| n has to stay below 2^107 (2^127). A row that sees a NaN or a logit of +inf is NaN in o and lse, and so are the weights that it
  * gives; a row all of whose logits are -inf is NaN in o. A NaN or infinity in v may also reach the rows of the tokens before it.
- * Outputs must not overlap inputs. Strides in elements, 0 = dense; q, k and v may be slices of one buffer. q, k, v, K, V, o must be 16-byte aligned, and so
- * must their strides in bytes; the other arrays 4-byte aligned.
+ * Outputs must not overlap inputs. Strides in elements, 0 = dense; q, k and v may be slices of one buffer. q, k, v, K, V, o must be
+ * 16-byte aligned, and so must their strides in bytes; the other arrays 4-byte aligned.
  *
  * Calls that write pages (append, evict, attend with mass) need pages that belong to one sequence each. Calls that only read
  * them do not: sequences may share pages.
  *
  * What only the device can see goes to the workspace's status word (caote_read_status): CAOTE_ERR_BAD_LENGTH (cu outside
  * [0, T], more than max_new new tokens, len outside [new tokens, max_pages * page_size]: the sequence is skipped; cu not ascending:
- * append moves no length on, the other calls' outputs mean nothing), CAOTE_ERR_BAD_PAGE (a page index outside [0, n_pages); nothing is read or written out of bounds; attend: the
- * outputs of that sequence and what its own tokens' weights grow by mean nothing, append: the sequence keeps its length, evict: it is skipped),
- * CAOTE_ERR_OVERFLOW as in caote.h.
+ * append moves no length on, the other calls' outputs mean nothing), CAOTE_ERR_BAD_PAGE (a page index outside [0, n_pages); nothing is
+ * read or written out of bounds, nor in other sequences' pages; attend: the outputs of that sequence and what its own tokens' weights
+ * grow by mean nothing, append: the sequence keeps its length, evict: it is skipped), CAOTE_ERR_OVERFLOW as in caote.h.
  */
 #ifndef CAOTE_PAGED_H_
 #define CAOTE_PAGED_H_
@@ -60,7 +60,9 @@ typedef struct {
 } caote_paged_params_t;
 
 /* Bytes of scratch for all calls below with these parameters; 0 if they are invalid. A workspace made for larger total_new
- * and max_new (everything else equal) serves smaller ones. Its first 256 bytes are as in caote_workspace_bytes. */
+ * and max_new (everything else equal) serves smaller ones. Its first 256 bytes are as in caote_workspace_bytes. With bf16 pages it holds
+ * the logits of up to 16 rows for every slot of the page table, batch * Hkv * max_pages * page_size * 32 (rows <= 8) or 64 bytes, so
+ * max_pages is best no larger than the longest cache needs. */
 CAOTE_API size_t caote_paged_workspace_bytes(const caote_paged_params_t* params);
 
 /* Causal attention inside every packed prompt (Sec. 2, prompt prefill): for token i of a prompt

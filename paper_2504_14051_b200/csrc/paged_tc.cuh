@@ -10,8 +10,9 @@
 //                   per lane, so that a thread sums 2^(s - lse) over the rows of its own key without any exchange.
 //   combine_kernel  adds up what the splits of a row's keys left, sum_kernel what the chunks of a key's rows left.
 //
-// Roundings: P is rounded to bf16 once (2^-9 of each weight at most, half of that on average, of random sign); o, of which it
-// is a weighted sum, is rounded to bf16 itself, so o's error against 64 bits is sqrt(2) of what the output's type costs.
+// Roundings: P is rounded to bf16 once (2^-8 of each weight at most, of random sign), since the product takes bf16 on both sides; o,
+// of which it is a weighted sum, is rounded to bf16 itself, so o's error against 64 bits is sqrt(2) of what the output's type costs at
+// most (measured: 1.04 to 1.11 of it).
 // Maximum, sum, O, lse and mass are fp32; the sum takes the numerators before they are rounded.
 //
 // A row that sees a NaN or a logit of +inf is NaN, and so are its statistic and the weights that it gives; a masked weight is
@@ -37,7 +38,7 @@ using namespace caote::tc;
 using ptx::tma_load_3d;
 
 constexpr int kLeastTiles = 4;  // key tiles per split
-constexpr int kPolyOf = 4;      // of so many pairs of exponentials one goes to the FMA pipe (none: 239, one of four: 230 us, 12 001 prompt tokens)
+constexpr int kPolyOf = 4;      // of so many pairs of exponentials one goes to the FMA pipe (none: 260, one of four: 242 us, 12 001 prompt tokens)
 template <int D>
 constexpr int kKStages = D == 128 ? 2 : 4;
 template <int D>
@@ -552,7 +553,7 @@ combine_kernel(PDims dm, Seqs sq, __nv_bfloat16* __restrict__ o, float* __restri
 // that copy and issue run ahead of the key threads across items; rows, statistics and S buffers are counted through.
 // Of a prompt the first keys are seen by all rows: where that is more than a third of an SM's share, the rows are cut into chunks
 // that are items of their own and leave partial sums, which sum_kernel adds up in order (whole calls, one prompt of 6 000 tokens, 64/8
-// heads: 1 025 us in one chunk, 861 in five; of 4 000, 32/2 heads: 688 and 297).
+// heads: 1 025 - 1 050 us in one chunk, 870 - 970 in five; of 4 000, 32/2 heads: 692 and 304 - 331).
 constexpr int kKeys = 2 * kTile;                       // keys per item
 constexpr int kKeyThreads = 2 * kKeys;                 // two threads per key: 64 rows of a row block each
 constexpr int kMassThreads = kKeyThreads + 128;        // + products, items and K, Q, statistics
