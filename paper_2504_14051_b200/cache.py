@@ -117,6 +117,8 @@ class PagedCache:
         self.page_size, self.n_pages, self.max_pages = page_size, n_pages, -(-max_tokens // page_size)
         self.batch, self.Hq, self.Hkv, self.d = batch, n_q_heads, n_kv_heads, head_dim
         self.scale = head_dim ** -0.5 if scale is None else scale
+        if batch * n_kv_heads * -(-self.max_pages * page_size // 16) >= 1 << 31:  # (attention would refuse what append has taken)
+            raise ValueError(f"PagedCache: {batch} sequences of up to {self.max_pages * page_size} tokens are more than 2^31 blocks of 16")
         shape = (n_pages, n_kv_heads, page_size)
         self.K = torch.zeros(shape + (head_dim,), dtype=dtype, device=dev)
         self.V = torch.zeros(shape + (head_dim,), dtype=dtype, device=dev)

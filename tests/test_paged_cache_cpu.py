@@ -107,6 +107,12 @@ def test_settings_that_an_eviction_would_refuse(calls, bad):
         cache(**bad)
 
 
+def test_more_slots_than_attention_takes(calls):
+    """Append takes them: the cache is refused when it is made."""
+    with pytest.raises(ValueError, match="blocks of 16"):
+        P.PagedCache(1 << 14, Hq, Hkv, D, 256, 1, 1 << 20, 1, IO, 10, device="cpu")
+
+
 def test_no_entry_names_a_page_of_another_sequence(calls):
     c = cache()
     g = torch.Generator().manual_seed(0)
