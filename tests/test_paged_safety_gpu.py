@@ -136,6 +136,7 @@ def test_weights_in_a_cache_of_more_than_2_27_tokens():
     assert abs(float(flat[-1]) - 16 / n) <= tol * 16 / n
 
 
+@pytest.mark.filterwarnings("ignore:The CUDA Graph is empty")
 def test_a_cache_refuses_to_be_captured_and_goes_on():
     c = P.PagedCache(1, 4, 2, 64, 16, 8, 100, 40, BF, 30)
     q, k, v = (torch.randn(40, h, 64, device=DEV).to(BF) for h in (4, 2, 2))
